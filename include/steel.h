@@ -336,6 +336,165 @@ int steel_attn_fwd_noalloc(const void* q, const void* k, const void* v,
                            int B, int Hq, int Hkv, int S_q, int S_k, int D, int blk,
                            float scale, int causal, void* stream);
 
+/*
+ * Paged 4-bit key/value cache: keys and values of many sequences in a pool of
+ * pages, attention that reads it, and the bookkeeping of its pages.
+ *
+ * Pool.  A page holds 64 tokens of every key/value head (the block edge of the
+ * masks above: a page is one key tile).  ``pages`` is uint8 [n_pages][Hkv][68 D],
+ * 16-byte aligned; the 68 D bytes of a page and a head are, in this order,
+ *   key codes [64][D/2]     token t, channels 2c (low nibble) and 2c + 1
+ *   value codes [64][D/2]
+ *   key scales [64][D/32], value scales [64][D/32]
+ * A code is an E2M1 number: bits 0-2 select 0 0.5 1 1.5 2 3 4 6, bit 3 is the
+ * sign.  A scale byte b stands for 2^(b - 127) and covers 32 channels of one
+ * token.  A stored vector x has, per 32 channels, the smallest scale 2^e with
+ * max |x| <= 6 * 2^e, e in [-125, 125], and codes x / 2^e rounded to nearest
+ * (ties to the even code, magnitudes above 6 to 6).  A vector with a NaN or an
+ * infinity has code 0 and scale bytes 255 throughout: all its values stand for
+ * NaN.  D is 64 or 128 (others: STEEL_ERR_UNSUPPORTED).
+ *
+ * Sequences.  page_table int32 [B][max_pages]: entry j of row b is the page of
+ * tokens 64 j .. 64 j + 63 of sequence b.  lens int32 [B]: the tokens that each
+ * sequence has.  Only entries j < ceil(lens[b] / 64) of a row are held; the
+ * others (-1 where the calls below write them) are not read as pages.  Tables, lengths, reference
+ * counts and page numbers are device memory and are read by the kernels: a
+ * page number outside [0, n_pages) is a page that does not exist (nothing is
+ * written to it, no key of it is visible), a length outside [0, 64 max_pages]
+ * counts as the nearer end of it where keys are read or pages held.
+ *
+ * n_new int32 [B], device, or NULL: how many of the S tokens (or S_q queries)
+ * of a padded batch sequence b has, at the front of its S (clamped to [0, S];
+ * NULL: all S).  lens counts them already: token or query i < n_new[b] stands at
+ * position lens[b] - n_new[b] + i.
+ *
+ * None of these calls allocates or waits for the host; all may be captured into a
+ * HIP graph.  Workspaces are the caller's: device memory, 256-byte aligned,
+ * contents arbitrary, in use until the call's work is done (two captured graphs
+ * that may run at one time need one each).
+ */
+
+/*
+ * Writes new keys and values into the cache.
+ *
+ *   k, v     bf16 [B][Hkv][S][D]: element (b, h, i, d) at b * sb + h * sh + i * ss
+ *            + d (strides in elements, multiples of 8, >= 0), 16-byte aligned
+ *   pages    see above; the tokens' slots are overwritten, all else is kept
+ *
+ * A token whose position is negative, whose entry lies past the table or whose page does
+ * not exist is dropped.  Two rows of one call that write the same slot (a shared
+ * page written without steel_pages_grow and steel_pages_copy) leave either's
+ * bytes in it.
+ */
+int steel_cache_append(const void* k, const void* v, long long k_sb, long long k_sh,
+                       long long k_ss, long long v_sb, long long v_sh, long long v_ss,
+                       uint8_t* pages, const int32_t* page_table, const int32_t* lens,
+                       const int32_t* n_new, int B, int Hkv, int S, int D, int max_pages,
+                       int n_pages, void* stream);
+
+/*
+ * Reads keys and values back as bf16 (exact: every value of the cache is a bf16
+ * number), for example to hand a cached prefix to steel_attn_fwd.
+ *
+ *   start    int32 [B], device, or NULL (0): first token of each sequence
+ *   k, v     bf16 [B][Hkv][S][D], 16-byte aligned: token start[b] + i at row i; rows
+ *            of tokens that do not exist are 0
+ */
+int steel_cache_load(const uint8_t* pages, const int32_t* page_table, const int32_t* lens,
+                     const int32_t* start, void* k, void* v, int B, int Hkv, int S, int D,
+                     int max_pages, int n_pages, void* stream);
+
+/*
+ * steel_attn_fwd_ex for queries against the cache: single tokens, drafted
+ * tokens, chunks of prompts.
+ *
+ *   q        bf16 [B][Hq][S_q][D] by strides as for steel_cache_append
+ *   out      [B][Hq][S_q][D], 16-byte aligned, fp32, or bf16 with
+ *            STEEL_OUT_BF16 (the only flag); every element is written
+ *   lse      float [B][Hq][S_q] or NULL: row log-sum-exp (natural log)
+ *   block_mask   uint8 [B][Hkv][max_pages], device, or NULL: pages with byte 0 are
+ *            not visible to the query heads of that key/value head
+ *   window_blocks, sink_blocks   window_blocks > 0: the structured mask of
+ *            steel_attn_fwd_window over blocks of 64 positions; 0: none
+ *   causal   0 or 1
+ *
+ * With p the position of query i (see n_new), key j of sequence b is visible iff
+ * 0 <= j < lens[b], p >= 0, (j <= p or not causal), its page exists and is live,
+ * and with a window p/64 - window_blocks < j/64 <= p/64 or j/64 < sink_blocks.
+ * Queries without a visible key, and queries i >= n_new[b], get out 0 and lse
+ * -inf.  A token whose keys or values stand for NaN makes the rows that see it
+ * NaN, and no others.  Rows are sums in fp32; the softmax weights are rounded
+ * to bf16 where they meet V.  Results are bitwise reproducible run to run.
+ *
+ *   workspace   at least steel_attn_cache_workspace_bytes of the same sizes
+ *               (0 after an argument error)
+ */
+size_t steel_attn_cache_workspace_bytes(int B, int Hq, int Hkv, int S_q, int D, int max_pages);
+
+int steel_attn_cache(const void* q, long long q_sb, long long q_sh, long long q_ss,
+                     const uint8_t* pages, const int32_t* page_table, const int32_t* lens,
+                     const int32_t* n_new, const uint8_t* block_mask, void* out, float* lse, int B,
+                     int Hq, int Hkv, int S_q, int D, int max_pages, int n_pages, float scale,
+                     int causal, int window_blocks, int sink_blocks, int flags, void* workspace,
+                     size_t workspace_bytes, void* stream);
+
+/*
+ * New rows of the page table from old ones: beams reordered, sequences forked
+ * (two rows with one parent share its pages) and freed (parent -1).
+ *
+ *   refs       int32 [n_pages]: rows that hold each page; 0 = free.  Updated: plus
+ *              one for every page that a new row holds, minus one for every
+ *              page that an old row held
+ *   parent     int32 [B_out]: the old row that new row b continues; anything outside
+ *              [0, B_in): an empty row
+ *   table_out, lens_out   the new rows [B_out][max_pages] and lengths; entries that a
+ *              row does not hold are -1.  They may not alias page_table and lens
+ */
+int steel_pages_fork(const int32_t* page_table, const int32_t* lens, int32_t* refs,
+                     const int32_t* parent, int32_t* table_out, int32_t* lens_out, int B_in,
+                     int B_out, int max_pages, int n_pages, void* stream);
+
+/*
+ * Room for n_new[b] more tokens of every sequence (negative: 0): lens grows, and
+ * rows take free pages, in increasing order of page number, row after row.  A row
+ * that writes into a last page which other rows hold too takes a page of its own in
+ * its place first and lets go of the shared one; of several such rows in one call
+ * the last keeps the page if no other row holds it then.  The bytes are not copied here:
+ * src[b] and dst[b] (int32 [B]) are the pages to copy for row b, or -1, for
+ * steel_pages_copy.
+ *   left       int32 [1]: free pages that remain.  Negative: that many were missing,
+ *              or INT32_MIN: a row would need more than max_pages entries; then
+ *              nothing has changed and every src and dst is -1
+ *   workspace  at least steel_pages_workspace_bytes
+ * n_pages up to 2^22.
+ */
+size_t steel_pages_workspace_bytes(int n_pages, int B);
+
+int steel_pages_grow(int32_t* page_table, int32_t* lens, int32_t* refs, const int32_t* n_new,
+                     int32_t* src, int32_t* dst, int32_t* left, int B, int max_pages, int n_pages,
+                     void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Copies page src[i] onto page dst[i] for i < n, in each of ``layers`` pools
+ * (layer l begins at pages + l * n_pages * page_bytes; page_bytes, a multiple of 16, is
+ * Hkv * 68 * D for a cache).  Pairs with a page number outside [0, n_pages) are
+ * skipped.  The destinations are distinct and no source: a page that is written
+ * twice, or read and written, has unspecified bytes afterwards.
+ */
+int steel_pages_copy(uint8_t* pages, const int32_t* src, const int32_t* dst, int n, int layers,
+                     int n_pages, size_t page_bytes, void* stream);
+
+/*
+ * Moves the live pages (refs > 0) to the front of the pool, in each of ``layers``
+ * pools: with n of them, those numbered n or more move, in order, to the free
+ * pages below n, in order.  page_table (the held entries) and refs follow.
+ *   live       int32 [1]: n
+ *   workspace  at least steel_pages_workspace_bytes
+ */
+int steel_pages_compact(uint8_t* pages, int32_t* page_table, const int32_t* lens, int32_t* refs,
+                        int32_t* live, int B, int max_pages, int layers, int n_pages,
+                        size_t page_bytes, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Text of the last non-OK status returned on the calling thread ("" if none). */
 const char* steel_last_error(void);
 

@@ -19,7 +19,9 @@ It is written from the paper's definitions, independently of the GPU code:
   merges partial results computed over disjoint key chunks;
 * ``fp8_attention`` -- a float64 model of the library's fp8 (E4M3) form:
   Algorithm 1's online recurrence with both products taking E4M3 operands
-  under power-of-two scales (an extension of Section II-C's bf16 datapath).
+  under power-of-two scales (an extension of Section II-C's bf16 datapath);
+* ``kv_cache``    -- the paged 4-bit key/value cache: its number format, attention
+  over it and the bookkeeping of its pages.
 
 Every function is pinned by tests against things other than itself: brute
 force on tiny inputs, closed forms, invariants and an independent library
@@ -30,3 +32,4 @@ from .block_index import N_BINS, build_index, count_bin, tile_classes, work_orde
 from .block_select import block_means, block_scores, keep_count, topk_meanpool_mask  # noqa: F401
 from .lse_merge import attention_lse, merge_partials  # noqa: F401
 from .fp8_attention import attention_fp8, e4m3_round, pow2_scale  # noqa: F401
+from . import kv_cache  # noqa: F401

@@ -71,6 +71,21 @@ def _check_bf16(name, t, ndim=4):
         raise ValueError(f"{name} must be contiguous")
 
 
+def _check_bf16_rows(name, t, device):
+    """A bf16 [B, H, S, D] tensor with contiguous rows on the device: its strides over
+    batch, head and row in elements (0 over a dimension of one)."""
+    torch = _torch()
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if t.dtype != torch.bfloat16 or t.dim() != 4:
+        raise ValueError(f"{name} must be bfloat16 [B, H, S, D] (got {t.dtype} {tuple(t.shape)})")
+    if t.device != device:
+        raise ValueError(f"{name} must be on {device} (got {t.device})")
+    if t.stride(3) != 1:
+        raise ValueError(f"rows of {name} must be contiguous (strides {t.stride()})")
+    return [0 if n == 1 else st for n, st in zip(t.shape[:3], t.stride()[:3])]
+
+
 def _check_out(out, shape, device):
     """A caller-supplied fp32 output: the kernels write every element of a
     contiguous [B, Hq, S_q, D] float32 buffer on q's device, nothing less."""
@@ -352,3 +367,7 @@ class Plan:
                 self.workspace.numel(), _stream_handle(stream))
         _lib.check(st)
         return out
+
+
+from .cache import (attn_cache, cache_append, cache_load, cache_pool, pages_compact,  # noqa: E402,F401
+                    pages_copy, pages_fork, pages_grow)

@@ -79,6 +79,28 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.steel_lds_rate.argtypes = [c_int, c_int, c_int, c_int, c_void_p, c_void_p, c_void_p]
     lib.steel_copy_rate.restype = c_int
     lib.steel_copy_rate.argtypes = [c_void_p, c_size_t, c_int, c_int, c_int, c_void_p, c_void_p, c_void_p]
+    c_ll = ctypes.c_longlong
+    lib.steel_cache_append.restype = c_int
+    lib.steel_cache_append.argtypes = [c_void_p] * 2 + [c_ll] * 6 + [c_void_p] * 4 + [c_int] * 6 \
+        + [c_void_p]
+    lib.steel_cache_load.restype = c_int
+    lib.steel_cache_load.argtypes = [c_void_p] * 6 + [c_int] * 6 + [c_void_p]
+    lib.steel_attn_cache_workspace_bytes.restype = c_size_t
+    lib.steel_attn_cache_workspace_bytes.argtypes = [c_int] * 6
+    lib.steel_attn_cache.restype = c_int
+    lib.steel_attn_cache.argtypes = [c_void_p] + [c_ll] * 3 + [c_void_p] * 7 + [c_int] * 7 \
+        + [c_float] + [c_int] * 4 + [c_void_p, c_size_t, c_void_p]
+    lib.steel_pages_fork.restype = c_int
+    lib.steel_pages_fork.argtypes = [c_void_p] * 6 + [c_int] * 4 + [c_void_p]
+    lib.steel_pages_workspace_bytes.restype = c_size_t
+    lib.steel_pages_workspace_bytes.argtypes = [c_int] * 2
+    lib.steel_pages_grow.restype = c_int
+    lib.steel_pages_grow.argtypes = [c_void_p] * 7 + [c_int] * 3 + [c_void_p, c_size_t, c_void_p]
+    lib.steel_pages_copy.restype = c_int
+    lib.steel_pages_copy.argtypes = [c_void_p] * 3 + [c_int] * 3 + [c_size_t, c_void_p]
+    lib.steel_pages_compact.restype = c_int
+    lib.steel_pages_compact.argtypes = [c_void_p] * 5 + [c_int] * 4 + [c_size_t, c_void_p, c_size_t,
+                                                                       c_void_p]
     lib.steel_last_error.restype = ctypes.c_char_p
     lib.steel_last_error.argtypes = []
     lib.steel_version.restype = ctypes.c_char_p

@@ -20,7 +20,8 @@ BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libsteel.so")
 SOURCES = ["steel_api.cpp", "block_index.hip", "block_select.hip", "attn_fwd.hip", "attn_ws.hip",
            "attn_half.hip", "quant_fp8.hip",
-           "attn_merge.hip", "noalloc.hip", "mfma_peak.hip"]
+           "attn_merge.hip", "noalloc.hip", "mfma_peak.hip",
+           "cache_store.hip", "cache_attn.hip", "cache_pages.hip"]
 ARCH = "gfx950"
 
 # Packed fp32 VALU forms are kept out of every code object: the compiler would
@@ -36,7 +37,8 @@ COMMON = [
 # 256 registers each hold no AGPR file.
 PER_SOURCE = {"attn_fwd.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
               "attn_half.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
-              "attn_ws.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
+              "attn_ws.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
+              "cache_attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
 
 
 def hipcc() -> str:

@@ -20,6 +20,7 @@
 #include <vector>
 
 #include "../../include/steel.h"
+#include "cache_common.h"
 #include "internal.h"
 
 namespace {
@@ -322,6 +323,69 @@ int fused_call(const steel::Problem& p, const void* q, const void* k, const void
   return re;
 }
 
+// Sizes shared by the calls on the paged cache.
+int check_cache(int B, int Hkv, int S, int D, int max_pages, int n_pages) {
+  if (B < 1 || Hkv < 1 || S < 1 || max_pages < 1 || n_pages < 1)
+    return fail(STEEL_ERR_INVALID_ARGUMENT,
+                "sizes must be >= 1 (B=%d Hkv=%d S=%d max_pages=%d n_pages=%d)", B, Hkv, S,
+                max_pages, n_pages);
+  if (D != 64 && D != 128) return fail(STEEL_ERR_UNSUPPORTED, "D=%d not supported (64 or 128)", D);
+  if (max_pages > (1 << 24))
+    return fail(STEEL_ERR_UNSUPPORTED, "max_pages=%d exceeds 2^24", max_pages);
+  if ((long long)B * Hkv > INT32_MAX || (long long)B * Hkv * S > ((long long)1 << 34))
+    return fail(STEEL_ERR_UNSUPPORTED, "B * Hkv * S = %d * %d * %d is too large", B, Hkv, S);
+  return STEEL_OK;
+}
+
+int check_cache_heads(int B, int Hq, int Hkv, int S_q, int D, int max_pages, int n_pages) {
+  const int rc = check_cache(B, Hkv, S_q, D, max_pages, n_pages);
+  if (rc != STEEL_OK) return rc;
+  if (Hq < 1 || Hq % Hkv != 0)
+    return fail(STEEL_ERR_INVALID_ARGUMENT, "Hq (%d) must be a multiple of Hkv (%d)", Hq, Hkv);
+  if ((long long)B * Hq * S_q > INT32_MAX / 2)
+    return fail(STEEL_ERR_UNSUPPORTED, "B * Hq * S_q = %d * %d * %d rows are too many", B, Hq, S_q);
+  return STEEL_OK;
+}
+
+// Strides of a [B][H][S][D] tensor with contiguous rows, in elements: rows stay
+// 16-byte aligned.
+int check_strides(const char* name, long long sb, long long sh, long long ss) {
+  if (sb < 0 || sh < 0 || ss < 0 || ((sb | sh | ss) & 7) != 0)
+    return fail(STEEL_ERR_INVALID_ARGUMENT,
+                "strides of %s must be >= 0 and multiples of 8 (got %lld, %lld, %lld)", name, sb,
+                sh, ss);
+  return STEEL_OK;
+}
+
+// Sizes shared by the calls on the page table.
+int check_pages(int B, int max_pages, int n_pages) {
+  if (B < 1 || max_pages < 1 || n_pages < 1)
+    return fail(STEEL_ERR_INVALID_ARGUMENT, "sizes must be >= 1 (B=%d max_pages=%d n_pages=%d)", B,
+                max_pages, n_pages);
+  if (max_pages > (1 << 24) || n_pages > steel::kMaxPages || (long long)B * max_pages > INT32_MAX)
+    return fail(STEEL_ERR_UNSUPPORTED,
+                "B=%d rows of max_pages=%d, n_pages=%d: too large (2^31 entries, 2^24 a row, %d pages)",
+                B, max_pages, n_pages, steel::kMaxPages);
+  return STEEL_OK;
+}
+
+int check_pool(const void* pages, int layers, int n_pages, size_t page_bytes) {
+  if (!pages || !aligned16(pages))
+    return fail(STEEL_ERR_INVALID_ARGUMENT, "pages must be a 16-byte aligned device pointer");
+  if (layers < 1 || layers > 65535 || page_bytes < 16 || page_bytes % 16 != 0 ||
+      page_bytes > ((size_t)1 << 30))
+    return fail(STEEL_ERR_INVALID_ARGUMENT,
+                "layers (%d) must be 1 .. 65535, page_bytes (%zu) a multiple of 16 up to 2^30", layers,
+                page_bytes);
+  return STEEL_OK;
+}
+
+int check_bytes(const void* ws, size_t bytes, size_t need) {
+  Layout L{};
+  L.total = need;
+  return check_workspace(ws, bytes, L);
+}
+
 }  // namespace
 
 extern "C" {
@@ -555,6 +619,181 @@ int steel_block_index(const uint8_t* block_mask, int B, int Hq, int S_q, int S_k
   const int re = scratch_end(slot, dev, s);
   if (e != hipSuccess) return hip_fail(e, "launching kernels");
   return re;
+}
+
+int steel_cache_append(const void* k, const void* v, long long k_sb, long long k_sh,
+                       long long k_ss, long long v_sb, long long v_sh, long long v_ss,
+                       uint8_t* pages, const int32_t* page_table, const int32_t* lens,
+                       const int32_t* n_new, int B, int Hkv, int S, int D, int max_pages,
+                       int n_pages, void* stream) {
+  g_err.clear();
+  int rc = check_cache(B, Hkv, S, D, max_pages, n_pages);
+  if (rc != STEEL_OK) return rc;
+  if (!k || !v || !pages || !page_table || !lens)
+    return fail(STEEL_ERR_INVALID_ARGUMENT, "k, v, pages, page_table and lens must be non-NULL");
+  if (!aligned16(k) || !aligned16(v) || !aligned16(pages))
+    return fail(STEEL_ERR_INVALID_ARGUMENT, "k, v and pages must be 16-byte aligned");
+  if ((rc = check_strides("k", k_sb, k_sh, k_ss)) != STEEL_OK) return rc;
+  if ((rc = check_strides("v", v_sb, v_sh, v_ss)) != STEEL_OK) return rc;
+  steel::StoreArgs a{static_cast<const __bf16*>(k), static_cast<const __bf16*>(v), k_sb, k_sh, k_ss,
+                     v_sb, v_sh, v_ss, pages, page_table, lens, n_new, B, Hkv, S, max_pages, n_pages};
+  const hipError_t e = steel::launch_cache_append(a, D, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? STEEL_OK : hip_fail(e, "launching the append");
+}
+
+int steel_cache_load(const uint8_t* pages, const int32_t* page_table, const int32_t* lens,
+                     const int32_t* start, void* k, void* v, int B, int Hkv, int S, int D,
+                     int max_pages, int n_pages, void* stream) {
+  g_err.clear();
+  const int rc = check_cache(B, Hkv, S, D, max_pages, n_pages);
+  if (rc != STEEL_OK) return rc;
+  if (!k || !v || !pages || !page_table || !lens)
+    return fail(STEEL_ERR_INVALID_ARGUMENT, "pages, page_table, lens, k and v must be non-NULL");
+  if (!aligned16(k) || !aligned16(v) || !aligned16(pages))
+    return fail(STEEL_ERR_INVALID_ARGUMENT, "pages, k and v must be 16-byte aligned");
+  steel::LoadArgs a{pages, page_table, lens, start, static_cast<__bf16*>(k), static_cast<__bf16*>(v),
+                    B, Hkv, S, max_pages, n_pages};
+  const hipError_t e = steel::launch_cache_load(a, D, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? STEEL_OK : hip_fail(e, "launching the load");
+}
+
+size_t steel_attn_cache_workspace_bytes(int B, int Hq, int Hkv, int S_q, int D, int max_pages) {
+  g_err.clear();
+  if (check_cache_heads(B, Hq, Hkv, S_q, D, max_pages, 1) != STEEL_OK) return 0;
+  return align256(steel::cache_attn_ws(B, Hq, Hkv, S_q, D, max_pages));
+}
+
+int steel_attn_cache(const void* q, long long q_sb, long long q_sh, long long q_ss,
+                     const uint8_t* pages, const int32_t* page_table, const int32_t* lens,
+                     const int32_t* n_new, const uint8_t* block_mask, void* out, float* lse, int B,
+                     int Hq, int Hkv, int S_q, int D, int max_pages, int n_pages, float scale,
+                     int causal, int window_blocks, int sink_blocks, int flags, void* workspace,
+                     size_t workspace_bytes, void* stream) {
+  g_err.clear();
+  int rc = check_cache_heads(B, Hq, Hkv, S_q, D, max_pages, n_pages);
+  if (rc != STEEL_OK) return rc;
+  if (!q || !pages || !page_table || !lens || !out)
+    return fail(STEEL_ERR_INVALID_ARGUMENT, "q, pages, page_table, lens and out must be non-NULL");
+  if (!aligned16(q) || !aligned16(pages) || !aligned16(out))
+    return fail(STEEL_ERR_INVALID_ARGUMENT, "q, pages and out must be 16-byte aligned");
+  if (!std::isfinite(scale) || !(scale > 0.f))
+    return fail(STEEL_ERR_INVALID_ARGUMENT, "scale must be finite and > 0 (got %g)", (double)scale);
+  if ((rc = check_strides("q", q_sb, q_sh, q_ss)) != STEEL_OK) return rc;
+  if (causal != 0 && causal != 1)
+    return fail(STEEL_ERR_INVALID_ARGUMENT, "causal must be 0 or 1 (got %d)", causal);
+  if (window_blocks < 0 || sink_blocks < 0)
+    return fail(STEEL_ERR_INVALID_ARGUMENT, "window_blocks (%d) and sink_blocks (%d) must be >= 0",
+                window_blocks, sink_blocks);
+  if (window_blocks == 0 && sink_blocks > 0)
+    return fail(STEEL_ERR_INVALID_ARGUMENT, "sink_blocks (%d) needs a window", sink_blocks);
+  if (flags & ~STEEL_OUT_BF16)
+    return fail(STEEL_ERR_INVALID_ARGUMENT, "flags may hold only STEEL_OUT_BF16 (got %d)", flags);
+  if ((rc = check_bytes(workspace, workspace_bytes,
+                        steel::cache_attn_ws(B, Hq, Hkv, S_q, D, max_pages))) != STEEL_OK)
+    return rc;
+  steel::CacheArgs a{};
+  a.q = static_cast<const __bf16*>(q);
+  a.q_sb = q_sb;
+  a.q_sh = q_sh;
+  a.q_ss = q_ss;
+  a.pages = pages;
+  a.table = page_table;
+  a.lens = lens;
+  a.fresh = n_new;
+  a.mask = block_mask;
+  a.out = out;
+  a.lse = lse;
+  a.out_bf16 = flags & STEEL_OUT_BF16 ? 1 : 0;
+  a.B = B;
+  a.Hq = Hq;
+  a.Hkv = Hkv;
+  a.G = Hq / Hkv;
+  a.S_q = S_q;
+  a.M = max_pages;
+  a.n_pages = n_pages;
+  a.causal = causal;
+  a.win = window_blocks;
+  a.sink = sink_blocks;
+  a.c = scale * 1.4426950408889634f;
+  const hipError_t e = steel::launch_cache_attn(a, D, workspace, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? STEEL_OK : hip_fail(e, "launching the attention kernels");
+}
+
+int steel_pages_fork(const int32_t* page_table, const int32_t* lens, int32_t* refs,
+                     const int32_t* parent, int32_t* table_out, int32_t* lens_out, int B_in,
+                     int B_out, int max_pages, int n_pages, void* stream) {
+  g_err.clear();
+  if (!page_table || !lens || !refs || !parent || !table_out || !lens_out)
+    return fail(STEEL_ERR_INVALID_ARGUMENT,
+                "page_table, lens, refs, parent, table_out and lens_out must be non-NULL");
+  if (page_table == table_out || lens == lens_out)
+    return fail(STEEL_ERR_INVALID_ARGUMENT, "table_out and lens_out may not alias page_table and lens");
+  int rc = check_pages(B_in, max_pages, n_pages);
+  if (rc == STEEL_OK) rc = check_pages(B_out, max_pages, n_pages);
+  if (rc != STEEL_OK) return rc;
+  const hipError_t e = steel::launch_pages_fork(page_table, lens, refs, parent, table_out, lens_out,
+                                                B_in, B_out, max_pages, n_pages,
+                                                static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? STEEL_OK : hip_fail(e, "launching the fork");
+}
+
+size_t steel_pages_workspace_bytes(int n_pages, int B) {
+  g_err.clear();
+  if (check_pages(B, 1, n_pages) != STEEL_OK) return 0;
+  return align256(sizeof(int32_t) * steel::pages_ws_ints(n_pages, B));
+}
+
+int steel_pages_grow(int32_t* page_table, int32_t* lens, int32_t* refs, const int32_t* n_new,
+                     int32_t* src, int32_t* dst, int32_t* left, int B, int max_pages, int n_pages,
+                     void* workspace, size_t workspace_bytes, void* stream) {
+  g_err.clear();
+  if (!page_table || !lens || !refs || !n_new || !src || !dst || !left)
+    return fail(STEEL_ERR_INVALID_ARGUMENT,
+                "page_table, lens, refs, n_new, src, dst and left must be non-NULL");
+  int rc = check_pages(B, max_pages, n_pages);
+  if (rc != STEEL_OK) return rc;
+  if ((rc = check_bytes(workspace, workspace_bytes,
+                        sizeof(int32_t) * steel::pages_ws_ints(n_pages, B))) != STEEL_OK)
+    return rc;
+  const hipError_t e = steel::launch_pages_grow(page_table, lens, refs, n_new, src, dst, left, B,
+                                                max_pages, n_pages, static_cast<int32_t*>(workspace),
+                                                static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? STEEL_OK : hip_fail(e, "launching the growth");
+}
+
+int steel_pages_copy(uint8_t* pages, const int32_t* src, const int32_t* dst, int n, int layers,
+                     int n_pages, size_t page_bytes, void* stream) {
+  g_err.clear();
+  if (!src || !dst) return fail(STEEL_ERR_INVALID_ARGUMENT, "src and dst must be non-NULL");
+  int rc = check_pool(pages, layers, n_pages, page_bytes);
+  if (rc != STEEL_OK) return rc;
+  if (n < 1 || n_pages < 1)
+    return fail(STEEL_ERR_INVALID_ARGUMENT, "n (%d) and n_pages (%d) must be >= 1", n, n_pages);
+  if ((long long)n * (long long)((page_bytes + 16383) / 16384) > INT32_MAX)
+    return fail(STEEL_ERR_UNSUPPORTED, "%d pages of %zu bytes in one call are too many", n, page_bytes);
+  const hipError_t e = steel::launch_pages_copy(pages, (long long)(page_bytes * (size_t)n_pages),
+                                                (long long)page_bytes, layers, src, dst, n, n_pages,
+                                                static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? STEEL_OK : hip_fail(e, "launching the copy");
+}
+
+int steel_pages_compact(uint8_t* pages, int32_t* page_table, const int32_t* lens, int32_t* refs,
+                        int32_t* live, int B, int max_pages, int layers, int n_pages,
+                        size_t page_bytes, void* workspace, size_t workspace_bytes, void* stream) {
+  g_err.clear();
+  if (!page_table || !lens || !refs || !live)
+    return fail(STEEL_ERR_INVALID_ARGUMENT, "page_table, lens, refs and live must be non-NULL");
+  int rc = check_pool(pages, layers, n_pages, page_bytes);
+  if (rc == STEEL_OK) rc = check_pages(B, max_pages, n_pages);
+  if (rc != STEEL_OK) return rc;
+  if ((rc = check_bytes(workspace, workspace_bytes,
+                        sizeof(int32_t) * steel::pages_ws_ints(n_pages, B))) != STEEL_OK)
+    return rc;
+  const hipError_t e = steel::launch_pages_compact(
+      pages, (long long)(page_bytes * (size_t)n_pages), (long long)page_bytes, layers, page_table,
+      lens, refs, live, B, max_pages, n_pages, static_cast<int32_t*>(workspace),
+      static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? STEEL_OK : hip_fail(e, "launching the compaction");
 }
 
 }  // extern "C"
