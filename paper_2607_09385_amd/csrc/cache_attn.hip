@@ -32,32 +32,33 @@ typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(3))) i32x2 lds_i32x2;
 
 // Rows r0 .. r1 - 1 of (b, g): their positions and the pages that any of them sees,
-// [0, a_len) and [b0, b0 + count - a_len).
+// [0, a_len) and [b0, b0 + count - a_len).  Positions are below 2^31 and, since a
+// negative length counts as 0, not below -S_q.
 struct Span {
-  int keys;              // keys that exist
-  long long first;       // position of query 0
-  int n;                 // queries of the sequence
-  long long pmin, pmax;  // positions of the rows
+  int keys;        // keys that exist
+  int first;       // position of query 0
+  int n;           // queries of the sequence
+  int pmin, pmax;  // positions of the rows
   int a_len, b0, count;
 };
 
 __device__ __forceinline__ Span make_span(const CacheArgs& a, int b, int r0, int r1) {
   Span s;
-  const int len = a.lens[b];
+  const int len = max(a.lens[b], 0);
   s.n = a.fresh == nullptr ? a.S_q : min(max(a.fresh[b], 0), a.S_q);
-  s.keys = (int)min((long long)max(len, 0), (long long)a.M * kBlk);
-  s.first = (long long)len - s.n;
+  s.keys = min(len, a.M * kBlk);
+  s.first = len - s.n;
   s.pmin = s.first + r0 / a.G;
   s.pmax = s.first + min((r1 - 1) / a.G, s.n - 1);
   s.a_len = s.b0 = s.count = 0;
   if (s.pmax < s.pmin || s.pmax < 0) return s;
   int kend = (s.keys + kBlk - 1) / kBlk;
-  if (a.causal) kend = (int)min((long long)kend, s.pmax / kBlk + 1);
+  if (a.causal) kend = min(kend, s.pmax / kBlk + 1);
   s.a_len = s.count = kend;
   if (a.win > 0) {
     s.a_len = min(a.sink, kend);
-    s.b0 = (int)max((long long)s.a_len, max(s.pmin, 0ll) / kBlk - a.win + 1);
-    s.count = s.a_len + max((int)min((long long)kend, s.pmax / kBlk + 1) - s.b0, 0);
+    s.b0 = max(s.a_len, max(s.pmin, 0) / kBlk - a.win + 1);
+    s.count = s.a_len + max(min(kend, s.pmax / kBlk + 1) - s.b0, 0);
   }
   return s;
 }
@@ -68,33 +69,44 @@ __device__ __forceinline__ int span_page(const Span& s, int i) {
 
 // Whether every row of the span sees every key of page kb.
 __device__ __forceinline__ bool page_full(const CacheArgs& a, const Span& s, int kb) {
-  bool full = s.pmin >= 0 && (kb + 1) * (long long)kBlk <= s.keys;
-  if (a.causal) full = full && (kb + 1) * (long long)kBlk - 1 <= s.pmin;
+  const int end = (kb + 1) * kBlk;
+  bool full = s.pmin >= 0 && end <= s.keys;
+  if (a.causal) full = full && end - 1 <= s.pmin;
   if (a.win > 0 && kb >= a.sink) full = full && kb <= s.pmin / kBlk && kb > s.pmax / kBlk - a.win;
   return full;
 }
 
-// Last key of page kb (0 .. 63, or -1) that the query at position pos sees.
-__device__ __forceinline__ int row_limit(const CacheArgs& a, const Span& s, long long pos, int kb) {
-  if (pos < 0) return -1;
-  if (a.win > 0 && kb >= a.sink && (kb > pos / kBlk || kb <= pos / kBlk - a.win)) return -1;
-  long long last = s.keys - 1;
+// Last key of page kb (0 .. 63, or negative: none) that the query at position pos sees.
+__device__ __forceinline__ int row_limit(const CacheArgs& a, const Span& s, int pos, int kb) {
+  int last = s.keys - 1;
   if (a.causal) last = min(last, pos);
-  return (int)max(min(last - (long long)kb * kBlk, 63ll), -1ll);
+  if (a.win > 0 && kb >= a.sink && (kb > pos / kBlk || kb <= pos / kBlk - a.win)) last = -1;
+  if (pos < 0) last = -1;
+  return min(last - kb * kBlk, 63);
 }
 
-// Maximum or sum over the lanes l % 16 (the four lane groups of a row).
+// Maximum and sum over the lanes l % 16 (the four lane groups of a row), added in the
+// same order on all of them.
 __device__ __forceinline__ float row_max(float x) {
-  x = fmaxf(x, __shfl_xor(x, 16));
-  return fmaxf(x, __shfl_xor(x, 32));
+  const unsigned u = __float_as_uint(x);
+  const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  return other_half_max(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
 }
 __device__ __forceinline__ float row_sum(float x) {
-  x += __shfl_xor(x, 16);
-  return x + __shfl_xor(x, 32);
+  const unsigned u = __float_as_uint(x);
+  const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  return half_pair_sum(__uint_as_float(r[0]) + __uint_as_float(r[1]));
 }
 
-__device__ __forceinline__ uint32_t bf16_bits(__bf16 x) {
-  return (uint32_t)__builtin_bit_cast(unsigned short, x);
+// Calls f(e) for the elements e of a lane's 16 scores (token 16 (e / 4) + 4 q4 + e % 4)
+// whose token is in the set.
+template <typename F>
+__device__ __forceinline__ void for_tokens(uint64_t set, int q4, F f) {
+  set >>= 4 * q4;
+  uint32_t lo = (uint32_t)set, hi = (uint32_t)(set >> 32);
+  asm volatile("" : "+v"(lo), "+v"(hi));  // tested where it is rarely needed, not ahead of the loop
+#pragma unroll
+  for (int e = 0; e < 16; ++e) f(e, ((e < 8 ? lo : hi) >> (16 * (e / 4 % 2) + e % 4) & 1) != 0);
 }
 
 // 8 codes and their scale as 8 bf16 values.
@@ -107,25 +119,500 @@ __device__ __forceinline__ bf16x8 decode8(uint32_t w, float sc) {
 }
 
 constexpr int kWaves = 4;
-constexpr int kRows = 16;
+constexpr float kTau = 8.f;  // see the running maximum below
 
 // One page's codes and scales of a wave, on their way to registers.
 template <int D>
 struct PageRegs {
-  static constexpr int KW = D / 32;  // dwords of K codes per lane and 16 tokens
-  uint32_t k[4][KW];
-  uint32_t v[4][KW];
+  typedef unsigned Codes __attribute__((ext_vector_type(D / 32)));  // of a lane and 16 tokens
+  Codes k0, k1, k2, k3, v0, v1, v2, v3;
   uint32_t ks, vs;  // scales of token `lane` (D / 32 bytes)
 };
 
+// How the live pages of a call are dealt to the workgroups: all lists one after
+// another in the order (sequence, key/value head, page), workgroup w takes units
+// [w U, (w + 1) U) of them.  A list that lies in more than one workgroup is joined
+// from partial results; a workgroup leaves at most two of them, slot 2 w for the
+// first list it touches and 2 w + 1 for the last.
+struct SplitArgs {
+  int groups;     // workgroups of the attention kernel
+  int least;      // units per workgroup at least
+  float* part;    // O [2 groups][rows][D], or nullptr: one workgroup per list, nothing is split
+  float* ml;      // {m, l} [2 groups][rows]
+};
+
+// Where the units of a call lie: computed by every workgroup from the lengths.
+struct Deal {
+  long long total;   // units of the call
+  long long unit;    // units per workgroup
+  int b;             // sequence asked for
+  long long before;  // units before it
+};
+
+// The sequence of this workgroup's first unit (seq < 0), or sequence seq.  Thread t counts
+// the sequences t per .. t per + per - 1, and the one that has the answer leaves it in LDS.
+__device__ __forceinline__ Deal make_deal(const CacheArgs& a, const SplitArgs& sa, int rows,
+                                          long long* lds, int seq) {
+  constexpr int T = 64 * kWaves;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int per = (a.B + T - 1) / T, b0 = tid * per, b1 = min(b0 + per, a.B);
+  long long mine = 0;
+  for (int b = b0; b < b1; ++b) mine += (long long)make_span(a, b, 0, rows).count * a.Hkv;
+  long long inc = mine;
+#pragma unroll
+  for (int o = 1; o < 64; o *= 2) {
+    const long long y = __shfl_up(inc, o);
+    if (lane >= o) inc += y;
+  }
+  if (lane == 63) lds[wave] = inc;
+  __syncthreads();
+  long long before = inc - mine, total = 0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    before += w < wave ? lds[w] : 0;
+    total += lds[w];
+  }
+  Deal d;
+  d.total = total;
+  d.unit = max((long long)sa.least, (total + sa.groups - 1) / sa.groups);
+  const long long want = (long long)blockIdx.x * d.unit;
+  if (seq < 0 ? want >= before && want < before + mine : seq >= b0 && seq < b1) {
+    for (int b = b0; b < b1; ++b) {
+      const long long n = (long long)make_span(a, b, 0, rows).count * a.Hkv;
+      if (seq < 0 ? want < before + n : b == seq) {
+        lds[kWaves] = b;
+        lds[kWaves + 1] = before;
+        break;
+      }
+      before += n;
+    }
+  }
+  __syncthreads();
+  d.b = (int)lds[kWaves];
+  d.before = lds[kWaves + 1];
+  return d;
+}
+
+// Row r of (b, g) whose sums are O / l with l the sum of the weights: out and lse.
+template <int EPT>
+__device__ __forceinline__ void store_row(const CacheArgs& a, const Span& sp, int D, int b, int g,
+                                          int r, int d0, const float* acc, float top, float den) {
+  const int qi = r / a.G, h = g * a.G + r % a.G;
+  const bool dead = qi >= sp.n || sp.first + qi < 0 || den == 0.f;
+  const float inv = dead ? 0.f : 1.f / den;
+  const size_t row = ((size_t)b * a.Hq + h) * a.S_q + qi;
+  if (a.out_bf16) {
+#pragma unroll
+    for (int e = 0; e < EPT; e += 4) {
+      bf16x4 v;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = (__bf16)(dead ? 0.f : acc[e + i] * inv);
+      *(bf16x4*)((__bf16*)a.out + row * D + d0 + e) = v;
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < EPT; e += 4) {
+      f32x4 v;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = dead ? 0.f : acc[e + i] * inv;
+      *(f32x4*)((float*)a.out + row * D + d0 + e) = v;
+    }
+  }
+  if (d0 == 0 && a.lse != nullptr)
+    a.lse[row] = dead ? -INFINITY : (top + __builtin_amdgcn_logf(den)) * 0.6931471805599453f;
+}
+
 }  // namespace
+
+// Few rows per key/value head (S_q G <= 16 NT): every row in one tile.  A workgroup's
+// waves take every fourth page of a list, each with a state of its own, joined at
+// the list's (or the workgroup's) end.
+template <int D, int NT>
+__global__ __launch_bounds__(64 * kWaves) void k_cache_token(CacheArgs a, SplitArgs sa) {
+  using R = Record<D>;
+  using Regs = PageRegs<D>;
+  using Codes = typename Regs::Codes;
+  constexpr int KW = D / 32;        // dwords of codes per lane and 16 tokens, K steps of 32 channels
+  constexpr int GR = D / 32;        // scale groups
+  constexpr int CT = D / 16;        // channel tiles of the output
+  constexpr int VROW = D / 2;       // bytes of a token's V codes
+  constexpr int OP = D + 4;         // padded output row in LDS
+  constexpr int kWaveBytes = 64 * VROW + 2 * 64 * GR * 4;
+  constexpr int kJoinBytes = kWaves * 16 * (OP + 2) * 4;
+  constexpr int kLds = kWaves * kWaveBytes > kJoinBytes ? kWaves * kWaveBytes : kJoinBytes;
+  __shared__ __attribute__((aligned(16))) char lds[kLds];
+
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int n = lane & 15, q4 = lane >> 4;
+  const int rows = a.S_q * a.G;
+
+  long long left;        // units of this workgroup
+  int b, g, off;         // list and page of the next one
+  bool split;
+  if (sa.part == nullptr) {
+    b = blockIdx.x / a.Hkv;
+    g = blockIdx.x % a.Hkv;
+    off = 0;
+    left = 1;  // one list, whatever its length
+    split = false;
+  } else {
+    const Deal d = make_deal(a, sa, rows, (long long*)lds, -1);
+    __syncthreads();
+    const long long lo = (long long)blockIdx.x * d.unit;
+    left = min(d.unit, d.total - lo);
+    if (left > 0) {
+      const int count = make_span(a, d.b, 0, rows).count;
+      b = d.b;
+      g = (int)((lo - d.before) / count);
+      off = (int)(lo - d.before - (long long)g * count);
+    } else {
+      b = g = off = 0;
+    }
+    split = true;
+    // lists without a page: their rows are zero
+    for (int z = blockIdx.x; z < a.B; z += sa.groups) {
+      const Span sp = make_span(a, z, 0, rows);
+      if (sp.count > 0) continue;
+      const float zero[4] = {0.f, 0.f, 0.f, 0.f};
+      for (int i = threadIdx.x; i < a.Hkv * rows * (D / 4); i += 64 * kWaves)
+        store_row<4>(a, sp, D, z, i / (D / 4) / rows, i / (D / 4) % rows, i % (D / 4) * 4, zero, 0.f, 0.f);
+    }
+  }
+
+  char* wv = lds + wave * kWaveBytes;         // V codes, swizzled
+  float* wks = (float*)(wv + 64 * VROW);      // K scales [group][token]
+  float* wvs = wks + 64 * GR;                 // V scales [group][token]
+
+  bool first = true;
+  for (; left > 0; first = false) {
+    const Span sp = make_span(a, b, 0, rows);
+    const int end = split ? (int)min((long long)sp.count, off + left) : sp.count;
+
+    // this lane's query rows, and its part of Q as the B operand
+    bf16x8 qf[NT][KW];
+    int pos[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      const int row = 16 * t + n, qi = row / a.G;
+      const bool real = row < rows && qi < sp.n;
+      pos[t] = real ? sp.first + qi : -1;
+#pragma unroll
+      for (int s = 0; s < KW; ++s) qf[t][s] = bf16x8{};
+      if (real) {
+        const __bf16* qp = a.q + b * a.q_sb + (g * a.G + row % a.G) * a.q_sh + qi * a.q_ss + q4 * (D / 4);
+#pragma unroll
+        for (int s = 0; s < KW; ++s) qf[t][s] = *(const bf16x8*)(qp + 8 * s);
+      }
+    }
+
+    f32x4 o[NT][CT];
+    float m[NT], ms[NT], l[NT];  // ms: m, or 0 before the first key
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+#pragma unroll
+      for (int c = 0; c < CT; ++c) o[t][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+      m[t] = -INFINITY;
+      ms[t] = l[t] = 0.f;
+    }
+
+    // page numbers of this wave's next 64 pages, one per lane; -1: no key of it is visible
+    int ids = -1, base = off + wave;
+    auto load_ids = [&](int from) {
+      const int i = from + kWaves * lane;
+      int id = -1;
+      if (i < end) {
+        const int kb = span_page(sp, i);
+        id = a.table[(size_t)b * a.M + kb];
+        if (id >= a.n_pages) id = -1;
+        if (a.mask != nullptr && a.mask[((size_t)b * a.Hkv + g) * a.M + kb] == 0) id = -1;
+      }
+      return id;
+    };
+    auto load_page = [&](int id, Regs& x) {
+      const uint8_t* rec = a.pages + ((size_t)max(id, 0) * a.Hkv + g) * R::kBytes;
+      const uint8_t* at = rec + n * R::kRow + q4 * 4 * KW;
+      x.k0 = *(const Codes*)at;
+      x.k1 = *(const Codes*)(at + 16 * R::kRow);
+      x.k2 = *(const Codes*)(at + 32 * R::kRow);
+      x.k3 = *(const Codes*)(at + 48 * R::kRow);
+      x.v0 = *(const Codes*)(at + R::kV);
+      x.v1 = *(const Codes*)(at + R::kV + 16 * R::kRow);
+      x.v2 = *(const Codes*)(at + R::kV + 32 * R::kRow);
+      x.v3 = *(const Codes*)(at + R::kV + 48 * R::kRow);
+      if constexpr (GR == 4) {
+        x.ks = *(const uint32_t*)(rec + R::kKs + 4 * lane);
+        x.vs = *(const uint32_t*)(rec + R::kVs + 4 * lane);
+      } else {
+        x.ks = *(const unsigned short*)(rec + R::kKs + 2 * lane);
+        x.vs = *(const unsigned short*)(rec + R::kVs + 2 * lane);
+      }
+    };
+
+    Regs x;
+    int id = -1;
+    if (base < end) {
+      ids = load_ids(base);
+      id = __builtin_amdgcn_readfirstlane(ids);
+      if (id >= 0) load_page(id, x);
+    }
+    for (int i = base; i < end; i += kWaves) {
+      const int cur = id;
+      Codes kc[4];
+      uint64_t k_nan = 0, v_nan = 0;  // tokens that stand for NaN
+      if (cur >= 0) {  // V and the scales to LDS
+        auto at = [&](int t) {  // 16 (D = 128) or 8 bytes, swizzled within the token's row
+          const int slot = D == 128 ? (q4 ^ (n >> 2)) * 16 : (q4 ^ ((n >> 3) | ((t & 1) << 1))) * 8;
+          return (Codes*)(wv + (16 * t + n) * VROW + slot);
+        };
+        *at(0) = x.v0;
+        *at(1) = x.v1;
+        *at(2) = x.v2;
+        *at(3) = x.v3;
+        // all scale bytes of a vector are 255, or none
+        k_nan = __builtin_amdgcn_ballot_w64((x.ks & 0xff) == kScaleNan);
+        v_nan = __builtin_amdgcn_ballot_w64((x.vs & 0xff) == kScaleNan);
+        const uint32_t vs = (x.vs & 0xff) == kScaleNan ? 0x7f7f7f7fu : x.vs;
+#pragma unroll
+        for (int gr = 0; gr < GR; ++gr) {
+          wks[64 * gr + lane] = __uint_as_float(((x.ks >> (8 * gr)) & 0xff) << 23);
+          wvs[64 * gr + lane] = __uint_as_float(((vs >> (8 * gr)) & 0xff) << 23);
+        }
+        kc[0] = x.k0;
+        kc[1] = x.k1;
+        kc[2] = x.k2;
+        kc[3] = x.k3;
+      }
+      if (i + kWaves < end) {  // the next page on its way
+        const int k = (i + kWaves - base) / kWaves;
+        if (k % 64 == 0) ids = load_ids(i + kWaves);
+        id = __builtin_amdgcn_readlane(ids, k % 64);
+        if (id >= 0) load_page(id, x);
+      }
+      if (cur < 0) continue;
+
+      // S^T: 4 tiles of 16 tokens
+      f32x4 sc[NT][4];
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        __builtin_amdgcn_sched_barrier(0);
+        const float ksc = wks[64 * (q4 * GR / 4) + 16 * t + n];
+#pragma unroll
+        for (int s = 0; s < KW; ++s) {
+          const bf16x8 kf = decode8(kc[t][s], ksc);
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+            sc[nt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                kf, qf[nt][s], s == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : sc[nt][t], 0, 0, 0);
+        }
+      }
+      if (k_nan != 0)
+        for_tokens(k_nan, q4, [&](int e, bool in) {
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) sc[nt][e / 4][e % 4] = in ? NAN : sc[nt][e / 4][e % 4];
+        });
+      const int kb = span_page(sp, i);
+      if (!page_full(a, sp, kb)) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          const int lim = row_limit(a, sp, pos[nt], kb) - 4 * q4;
+#pragma unroll
+          for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) sc[nt][t][r] = 16 * t + r > lim ? -INFINITY : sc[nt][t][r];
+        }
+      }
+      // The running maximum moves only where a row's scores exceed it by 2^kTau: m
+      // cancels in O / l, and weights up to 2^8 lose nothing in bf16.
+      bool grow = false;
+      float mx[NT];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        mx[nt] = sc[nt][0][0];
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) mx[nt] = fmaxf(mx[nt], sc[nt][t][r]);
+        grow |= mx[nt] * a.c > m[nt] + kTau;
+      }
+      if (__builtin_amdgcn_ballot_w64(grow)) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          const float mnew = fmaxf(m[nt], row_max(mx[nt]) * a.c);
+          ms[nt] = mnew == -INFINITY ? 0.f : mnew;
+          const float alpha = __builtin_amdgcn_exp2f(m[nt] - ms[nt]);  // 0 before the first key
+          m[nt] = mnew;
+          l[nt] *= alpha;
+#pragma unroll
+          for (int c = 0; c < CT; ++c) o[nt][c] *= alpha;
+        }
+      }
+      float p[NT][16];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          p[nt][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[nt][e / 4][e % 4], a.c, -ms[nt]));
+          l[nt] += p[nt][e];
+        }
+      if (v_nan != 0)  // rows that see such a token, and no others
+        for_tokens(v_nan, q4, [&](int e, bool in) {
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+            p[nt][e] = in && sc[nt][e / 4][e % 4] != -INFINITY ? NAN : p[nt][e];
+        });
+      // O^T += V^T P^T, 32 channels (one scale per token) at a time
+#pragma unroll
+      for (int gr = 0; gr < GR; ++gr) {
+        __builtin_amdgcn_sched_barrier(0);  // else all groups' operands are held at one time
+        f32x4 sv[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) sv[t] = *(const f32x4*)(wvs + 64 * gr + 16 * t + 4 * q4);
+        bf16x8 pf[NT][2];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            pf[nt][e / 8][e % 8] = (__bf16)(p[nt][e] * sv[e / 4][e % 4]);
+#pragma unroll
+        for (int c2 = 0; c2 < 2; ++c2) {
+          const int ct = 2 * gr + c2;
+          const int tok = 16 * (n >> 2) + 4 * q4 + (n & 3);
+          const int slot = D == 128 ? ((ct >> 1) ^ q4) * 16 + (ct & 1) * 8
+                                    : (ct ^ ((q4 >> 1) | (((n >> 2) & 1) << 1))) * 8;
+          const i32x2 w = __builtin_amdgcn_ds_read_tr4_b64_v2i32((lds_i32x2*)(wv + tok * VROW + slot));
+          const bf16x8 v0 = decode8((uint32_t)w[0], 1.f), v1 = decode8((uint32_t)w[1], 1.f);
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) {
+            o[nt][ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, pf[nt][0], o[nt][ct], 0, 0, 0);
+            o[nt][ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, pf[nt][1], o[nt][ct], 0, 0, 0);
+          }
+        }
+      }
+    }
+
+    // the waves' states of a row joined, then the rows or a partial result stored
+    const bool whole = off == 0 && end == sp.count;
+    const size_t slot = 2 * (size_t)blockIdx.x + (first ? 0 : 1);
+    float* jo = (float*)lds;              // [wave][16][OP]
+    float* jml = jo + kWaves * 16 * OP;   // [wave][16][2]
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      __syncthreads();
+      const float ls = row_sum(l[nt]);
+#pragma unroll
+      for (int c = 0; c < CT; ++c) *(f32x4*)(jo + (wave * 16 + n) * OP + 16 * c + 4 * q4) = o[nt][c];
+      if (q4 == 0) {
+        jml[(wave * 16 + n) * 2] = m[nt];
+        jml[(wave * 16 + n) * 2 + 1] = ls;
+      }
+      __syncthreads();
+      constexpr int TPR = 64 * kWaves / 16;     // threads per row
+      constexpr int EPT = D / TPR;              // elements per thread
+      const int jr = threadIdx.x / TPR, d0 = threadIdx.x % TPR * EPT, r = 16 * nt + jr;
+      if (r < rows) {
+        float top = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) top = fmaxf(top, jml[(w * 16 + jr) * 2]);
+        const float ts = top == -INFINITY ? 0.f : top;
+        float den = 0.f, acc[EPT];
+#pragma unroll
+        for (int e = 0; e < EPT; ++e) acc[e] = 0.f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+          const float f = __builtin_amdgcn_exp2f(jml[(w * 16 + jr) * 2] - ts);
+          den += f * jml[(w * 16 + jr) * 2 + 1];
+#pragma unroll
+          for (int e = 0; e < EPT; ++e) acc[e] += f * jo[(w * 16 + jr) * OP + d0 + e];
+        }
+        if (whole) {
+          store_row<EPT>(a, sp, D, b, g, r, d0, acc, ts, den);
+        } else {
+#pragma unroll
+          for (int e = 0; e < EPT; e += 4)
+            *(f32x4*)(sa.part + (slot * rows + r) * D + d0 + e) = f32x4{acc[e], acc[e + 1], acc[e + 2], acc[e + 3]};
+          if (d0 == 0) {
+            sa.ml[(slot * rows + r) * 2] = top;
+            sa.ml[(slot * rows + r) * 2 + 1] = den;
+          }
+        }
+      }
+    }
+    __syncthreads();
+
+    if (!split) break;
+    left -= end - off;
+    off = 0;
+    if (++g == a.Hkv) {
+      g = 0;
+      do ++b;
+      while (b < a.B && make_span(a, b, 0, rows).count == 0);
+      if (b >= a.B) break;
+    }
+  }
+}
+
+// Lists that lie in more than one workgroup of k_cache_token: their partial results
+// joined.  One workgroup per list and row; 8 (D = 128) or 16 threads of a column of 4
+// channels share the parts.
+template <int D>
+__global__ __launch_bounds__(64 * kWaves) void k_cache_join(CacheArgs a, SplitArgs sa) {
+  constexpr int C = D / 4, PG = 64 * kWaves / C;
+  __shared__ __attribute__((aligned(16))) f32x4 lds[PG][C];
+  __shared__ float ldsl[PG], ldsm[PG];
+  const int rows = a.S_q * a.G, b = blockIdx.x / a.Hkv, g = blockIdx.x % a.Hkv, r = blockIdx.y;
+  const Span sp = make_span(a, b, 0, rows);
+  if (sp.count == 0) return;  // uniform over the workgroup
+  const Deal d = make_deal(a, sa, rows, (long long*)lds, b);
+  __syncthreads();
+  const long long lo = d.before + (long long)g * sp.count;
+  const int w0 = (int)(lo / d.unit), w1 = (int)((lo + sp.count - 1) / d.unit);
+  if (w0 == w1) return;  // stored by its workgroup
+  const int first = 2 * w0 + (lo == w0 * d.unit ? 0 : 1);
+  const int c = threadIdx.x % C, pg = threadIdx.x / C;
+  auto slot_of = [&](int i) { return ((size_t)(i == 0 ? first : 2 * (w0 + i)) * rows + r); };
+  const int parts = w1 - w0 + 1;
+  float m = -INFINITY;
+  for (int i = pg; i < parts; i += PG) m = fmaxf(m, sa.ml[slot_of(i) * 2]);
+  if (c == 0) ldsm[pg] = m;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < PG; ++i) m = fmaxf(m, ldsm[i]);
+  const float ms = m == -INFINITY ? 0.f : m;
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  float l = 0.f;
+  for (int i = pg; i < parts; i += PG) {
+    const size_t at = slot_of(i);
+    const float f = __builtin_amdgcn_exp2f(sa.ml[at * 2] - ms);
+    l += f * sa.ml[at * 2 + 1];
+    acc += f * *(const f32x4*)(sa.part + at * D + 4 * c);
+  }
+  lds[pg][c] = acc;
+  if (c == 0) ldsl[pg] = l;
+  __syncthreads();
+  if (pg != 0) return;
+#pragma unroll
+  for (int i = 1; i < PG; ++i) {
+    acc += lds[i][c];
+    l += ldsl[i];
+  }
+  const float out[4] = {acc[0], acc[1], acc[2], acc[3]};
+  store_row<4>(a, sp, D, b, g, r, 4 * c, out, ms, l);
+}
+
+constexpr int kRows = 16;
+template <int D>
+struct TileRegs {
+  static constexpr int KW = D / 32;
+  uint32_t k[4][KW], v[4][KW], ks, vs;
+};
+
 
 // One workgroup per (sequence, key/value head, 16 rows); its waves take every
 // fourth live page, each with a state of its own, joined at the end.
 template <int D>
 __global__ __launch_bounds__(64 * kWaves) void k_cache_attn(CacheArgs a, int tiles) {
   using R = Record<D>;
-  using Regs = PageRegs<D>;
+  using Regs = TileRegs<D>;
   constexpr int KW = Regs::KW;      // also: K steps of 32 channels
   constexpr int GR = D / 32;        // scale groups
   constexpr int CT = D / 16;        // channel tiles of the output
@@ -146,7 +633,7 @@ __global__ __launch_bounds__(64 * kWaves) void k_cache_attn(CacheArgs a, int til
   // this lane's query row, and its part of Q as the B operand
   const int row = r0 + n, qi = row / a.G, h = g * a.G + row % a.G;
   const bool real = row < r1 && qi < sp.n;
-  const long long pos = real ? sp.first + qi : -1;
+  const int pos = real ? sp.first + qi : -1;
   bf16x8 qf[KW];
 #pragma unroll
   for (int s = 0; s < KW; ++s) qf[s] = bf16x8{};
@@ -316,10 +803,57 @@ __global__ __launch_bounds__(64 * kWaves) void k_cache_attn(CacheArgs a, int til
     a.lse[orow] = dead ? -INFINITY : (ts + __builtin_amdgcn_logf(den)) * 0.6931471805599453f;
 }
 
-size_t cache_attn_ws(int B, int Hq, int Hkv, int S_q, int D, int M) { return 256; }
+// What a call's sizes make of it.
+struct TokenPlan {
+  int groups;  // workgroups
+  bool split;
+  size_t part, ml, total;  // workspace offsets and size in bytes
+};
+
+TokenPlan token_plan(int B, int Hkv, int rows, int D, int M) {
+  TokenPlan p{};
+  const long long lists = (long long)B * Hkv, most = lists * M;
+  const long long want = (most + 3) / 4;
+  p.groups = (int)(want < 1024 ? want : 1024);
+  p.split = M > 16;
+  if (!p.split) p.groups = (int)lists;
+  p.ml = 0;
+  const size_t slots = 2 * (size_t)p.groups * rows;
+  p.part = (slots * 2 * sizeof(float) + 255) & ~(size_t)255;
+  p.total = p.split ? p.part + slots * D * sizeof(float) : 256;
+  return p;
+}
+
+template <int D>
+void launch_token(const CacheArgs& a, const SplitArgs& sa, int groups, int rows, hipStream_t s) {
+  const dim3 grid(groups), wg(64 * kWaves);
+  if (rows <= 16) hipLaunchKernelGGL((k_cache_token<D, 1>), grid, wg, 0, s, a, sa);
+  else if (rows <= 32) hipLaunchKernelGGL((k_cache_token<D, 2>), grid, wg, 0, s, a, sa);
+  else hipLaunchKernelGGL((k_cache_token<D, 4>), grid, wg, 0, s, a, sa);
+  if (sa.part != nullptr) hipLaunchKernelGGL(k_cache_join<D>, dim3(a.B * a.Hkv, rows), wg, 0, s, a, sa);
+}
+
+size_t cache_attn_ws(int B, int Hq, int Hkv, int S_q, int D, int M) {
+  const int rows = S_q * (Hq / Hkv);
+  return rows <= 64 ? token_plan(B, Hkv, rows, D, M).total : 256;
+}
 
 hipError_t launch_cache_attn(const CacheArgs& a, int D, void* ws, hipStream_t s) {
-  const int tiles = (a.S_q * a.G + kRows - 1) / kRows;
+  const int rows = a.S_q * a.G;
+  if (rows <= 64) {
+    const TokenPlan p = token_plan(a.B, a.Hkv, rows, D, a.M);
+    SplitArgs sa{};
+    sa.groups = p.groups;
+    sa.least = 4;
+    if (p.split) {
+      sa.ml = (float*)((char*)ws + p.ml);
+      sa.part = (float*)((char*)ws + p.part);
+    }
+    if (D == 64) launch_token<64>(a, sa, p.groups, rows, s);
+    else launch_token<128>(a, sa, p.groups, rows, s);
+    return hipGetLastError();
+  }
+  const int tiles = (rows + kRows - 1) / kRows;
   const dim3 grid((unsigned)(a.B * a.Hkv * tiles));
   if (D == 64)
     hipLaunchKernelGGL(k_cache_attn<64>, grid, dim3(64 * kWaves), 0, s, a, tiles);
