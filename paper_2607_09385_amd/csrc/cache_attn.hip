@@ -228,7 +228,7 @@ __device__ __forceinline__ void store_row(const CacheArgs& a, const Span& sp, in
 // waves take every fourth page of a list, each with a state of its own, joined at
 // the list's (or the workgroup's) end.
 template <int D, int NT>
-__global__ __launch_bounds__(64 * kWaves) void k_cache_token(CacheArgs a, SplitArgs sa) {
+__global__ __launch_bounds__(64 * kWaves, NT == 1 ? 3 : NT == 2 ? 2 : 1) void k_cache_token(CacheArgs a, SplitArgs sa) {
   using R = Record<D>;
   using Regs = PageRegs<D>;
   using Codes = typename Regs::Codes;
@@ -328,17 +328,17 @@ __global__ __launch_bounds__(64 * kWaves) void k_cache_token(CacheArgs a, SplitA
       }
       return id;
     };
-    auto load_page = [&](int id, Regs& x) {
-      const uint8_t* rec = a.pages + ((size_t)max(id, 0) * a.Hkv + g) * R::kBytes;
+    auto record = [&](int id) { return a.pages + ((size_t)id * a.Hkv + g) * R::kBytes; };
+    Regs x;
+    auto load_k = [&](const uint8_t* rec) {
       const uint8_t* at = rec + n * R::kRow + q4 * 4 * KW;
       x.k0 = *(const Codes*)at;
       x.k1 = *(const Codes*)(at + 16 * R::kRow);
       x.k2 = *(const Codes*)(at + 32 * R::kRow);
       x.k3 = *(const Codes*)(at + 48 * R::kRow);
-      x.v0 = *(const Codes*)(at + R::kV);
-      x.v1 = *(const Codes*)(at + R::kV + 16 * R::kRow);
-      x.v2 = *(const Codes*)(at + R::kV + 32 * R::kRow);
-      x.v3 = *(const Codes*)(at + R::kV + 48 * R::kRow);
+    };
+    auto load_v = [&](const uint8_t* rec) {
+      const uint8_t* at = rec + R::kV + n * R::kRow + q4 * 4 * KW;
       if constexpr (GR == 4) {
         x.ks = *(const uint32_t*)(rec + R::kKs + 4 * lane);
         x.vs = *(const uint32_t*)(rec + R::kVs + 4 * lane);
@@ -346,20 +346,23 @@ __global__ __launch_bounds__(64 * kWaves) void k_cache_token(CacheArgs a, SplitA
         x.ks = *(const unsigned short*)(rec + R::kKs + 2 * lane);
         x.vs = *(const unsigned short*)(rec + R::kVs + 2 * lane);
       }
+      x.v0 = *(const Codes*)at;
+      x.v1 = *(const Codes*)(at + 16 * R::kRow);
+      x.v2 = *(const Codes*)(at + 32 * R::kRow);
+      x.v3 = *(const Codes*)(at + 48 * R::kRow);
     };
 
-    Regs x;
     int id = -1;
     if (base < end) {
       ids = load_ids(base);
       id = __builtin_amdgcn_readfirstlane(ids);
-      if (id >= 0) load_page(id, x);
+      load_v(record(max(id, 0)));
+      load_k(record(max(id, 0)));
     }
     for (int i = base; i < end; i += kWaves) {
-      const int cur = id;
-      Codes kc[4];
-      uint64_t k_nan = 0, v_nan = 0;  // tokens that stand for NaN
-      if (cur >= 0) {  // V and the scales to LDS
+      const bool there = id >= 0;  // else page 0 stands in, none of its keys visible
+      // V and the scales to LDS
+      {
         auto at = [&](int t) {  // 16 (D = 128) or 8 bytes, swizzled within the token's row
           const int slot = D == 128 ? (q4 ^ (n >> 2)) * 16 : (q4 ^ ((n >> 3) | ((t & 1) << 1))) * 8;
           return (Codes*)(wv + (16 * t + n) * VROW + slot);
@@ -368,27 +371,24 @@ __global__ __launch_bounds__(64 * kWaves) void k_cache_token(CacheArgs a, SplitA
         *at(1) = x.v1;
         *at(2) = x.v2;
         *at(3) = x.v3;
-        // all scale bytes of a vector are 255, or none
-        k_nan = __builtin_amdgcn_ballot_w64((x.ks & 0xff) == kScaleNan);
-        v_nan = __builtin_amdgcn_ballot_w64((x.vs & 0xff) == kScaleNan);
-        const uint32_t vs = (x.vs & 0xff) == kScaleNan ? 0x7f7f7f7fu : x.vs;
-#pragma unroll
-        for (int gr = 0; gr < GR; ++gr) {
-          wks[64 * gr + lane] = __uint_as_float(((x.ks >> (8 * gr)) & 0xff) << 23);
-          wvs[64 * gr + lane] = __uint_as_float(((vs >> (8 * gr)) & 0xff) << 23);
-        }
-        kc[0] = x.k0;
-        kc[1] = x.k1;
-        kc[2] = x.k2;
-        kc[3] = x.k3;
       }
-      if (i + kWaves < end) {  // the next page on its way
-        const int k = (i + kWaves - base) / kWaves;
+      // all scale bytes of a vector are 255, or none: tokens that stand for NaN
+      const uint64_t k_nan = __builtin_amdgcn_ballot_w64((x.ks & 0xff) == kScaleNan);
+      const uint64_t v_nan = __builtin_amdgcn_ballot_w64((x.vs & 0xff) == kScaleNan);
+      const uint32_t vs = (x.vs & 0xff) == kScaleNan ? 0x7f7f7f7fu : x.vs;
+#pragma unroll
+      for (int gr = 0; gr < GR; ++gr) {
+        wks[64 * gr + lane] = __uint_as_float(((x.ks >> (8 * gr)) & 0xff) << 23);
+        wvs[64 * gr + lane] = __uint_as_float(((vs >> (8 * gr)) & 0xff) << 23);
+      }
+      // the next page on its way: V and scales here, K behind its last use
+      const int k = (i + kWaves - base) / kWaves;
+      if (i + kWaves < end) {
         if (k % 64 == 0) ids = load_ids(i + kWaves);
         id = __builtin_amdgcn_readlane(ids, k % 64);
-        if (id >= 0) load_page(id, x);
       }
-      if (cur < 0) continue;
+      const uint8_t* next = record(max(id, 0));
+      load_v(next);
 
       // S^T: 4 tiles of 16 tokens
       f32x4 sc[NT][4];
@@ -398,23 +398,24 @@ __global__ __launch_bounds__(64 * kWaves) void k_cache_token(CacheArgs a, SplitA
         const float ksc = wks[64 * (q4 * GR / 4) + 16 * t + n];
 #pragma unroll
         for (int s = 0; s < KW; ++s) {
-          const bf16x8 kf = decode8(kc[t][s], ksc);
+          const bf16x8 kf = decode8((t == 0 ? x.k0 : t == 1 ? x.k1 : t == 2 ? x.k2 : x.k3)[s], ksc);
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
             sc[nt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
                 kf, qf[nt][s], s == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : sc[nt][t], 0, 0, 0);
         }
       }
+      load_k(next);
       if (k_nan != 0)
         for_tokens(k_nan, q4, [&](int e, bool in) {
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) sc[nt][e / 4][e % 4] = in ? NAN : sc[nt][e / 4][e % 4];
         });
       const int kb = span_page(sp, i);
-      if (!page_full(a, sp, kb)) {
+      if (!there || !page_full(a, sp, kb)) {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-          const int lim = row_limit(a, sp, pos[nt], kb) - 4 * q4;
+          const int lim = there ? row_limit(a, sp, pos[nt], kb) - 4 * q4 : -1;
 #pragma unroll
           for (int t = 0; t < 4; ++t)
 #pragma unroll
@@ -446,6 +447,16 @@ __global__ __launch_bounds__(64 * kWaves) void k_cache_token(CacheArgs a, SplitA
           for (int c = 0; c < CT; ++c) o[nt][c] *= alpha;
         }
       }
+      uint32_t poison[NT];  // this lane's weights of values that stand for NaN, seen by their rows
+      if (v_nan != 0) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) poison[nt] = 0;
+        for_tokens(v_nan, q4, [&](int e, bool in) {
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+            poison[nt] |= in && sc[nt][e / 4][e % 4] != -INFINITY ? 1u << e : 0u;
+        });
+      }
       float p[NT][16];
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
@@ -454,12 +465,14 @@ __global__ __launch_bounds__(64 * kWaves) void k_cache_token(CacheArgs a, SplitA
           p[nt][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[nt][e / 4][e % 4], a.c, -ms[nt]));
           l[nt] += p[nt][e];
         }
-      if (v_nan != 0)  // rows that see such a token, and no others
-        for_tokens(v_nan, q4, [&](int e, bool in) {
+      if (v_nan != 0) {
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
-            p[nt][e] = in && sc[nt][e / 4][e % 4] != -INFINITY ? NAN : p[nt][e];
-        });
+        for (int nt = 0; nt < NT; ++nt) {
+          asm volatile("" : "+v"(poison[nt]));
+#pragma unroll
+          for (int e = 0; e < 16; ++e) p[nt][e] = poison[nt] >> e & 1 ? NAN : p[nt][e];
+        }
+      }
       // O^T += V^T P^T, 32 channels (one scale per token) at a time
 #pragma unroll
       for (int gr = 0; gr < GR; ++gr) {
@@ -814,7 +827,8 @@ TokenPlan token_plan(int B, int Hkv, int rows, int D, int M) {
   TokenPlan p{};
   const long long lists = (long long)B * Hkv, most = lists * M;
   const long long want = (most + 3) / 4;
-  p.groups = (int)(want < 1024 ? want : 1024);
+  const int most_groups = 256 * (rows <= 16 ? 3 : rows <= 32 ? 2 : 1);
+  p.groups = (int)(want < most_groups ? want : most_groups);
   p.split = M > 16;
   if (!p.split) p.groups = (int)lists;
   p.ml = 0;
