@@ -29,6 +29,8 @@ namespace {
 
 typedef int i32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(3))) i32x2 lds_i32x2;
 
 // Rows r0 .. r1 - 1 of (b, g): their positions and the pages that any of them sees,
@@ -109,6 +111,12 @@ __device__ __forceinline__ void for_tokens(uint64_t set, int q4, F f) {
   for (int e = 0; e < 16; ++e) f(e, ((e < 8 ? lo : hi) >> (16 * (e / 4 % 2) + e % 4) & 1) != 0);
 }
 
+// Two numbers rounded to bf16, in one register.
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{a, b}), bf16x2));
+}
+
 // 8 codes and their scale as 8 bf16 values.
 __device__ __forceinline__ bf16x8 decode8(uint32_t w, float sc) {
   const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, sc, 0);
@@ -118,20 +126,125 @@ __device__ __forceinline__ bf16x8 decode8(uint32_t w, float sc) {
   return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
+// The thread number, computed where it stands: what follows from it at a list's end then
+// holds no register over the pages.
+__device__ __forceinline__ int thread_here() {
+  int t = threadIdx.x;
+  asm volatile("" : "+v"(t));
+  return t;
+}
+
 constexpr int kWaves = 4;
+// Workgroups of k_cache_token per CU (one wave on each SIMD).
+constexpr int waves_per_simd(int D, int NT) { return NT == 1 ? 3 : 2; }
 constexpr float kTau = 8.f;  // see the running maximum below
 
-// One page's codes and scales of a wave, on their way to registers.
-template <int D>
+// One page's K codes and scales of a wave, on their way to registers.
 struct PageRegs {
-  typedef unsigned Codes __attribute__((ext_vector_type(D / 32)));  // of a lane and 16 tokens
-  Codes k0, k1, k2, k3, v0, v1, v2, v3;
-  uint32_t ks, vs;  // scales of token `lane` (D / 32 bytes)
+  u32x4 k0, k1, k2, k3;
+  uint32_t ks0, ks1, ks2, ks3;  // scales of the lane's K codes
+  uint32_t vs;                  // V scales of token `lane` (D / 32 bytes)
 };
 
+// Q of a lane's row as the fp8 operands of K Q^T: per 32 channels q = 2^e hi + 2^(e - 4) lo
+// with 2^e the smallest power of two that brings |q| to 448 or less, hi = q / 2^e and lo the
+// rest times 16, both rounded to E4M3.  hi has 4 significant bits and lo the next 4, so a
+// bf16 q is represented exactly down to 2^-14 of the 32's largest, and smaller ones to
+// 2^-22 of it.  D = 128: h holds hi of 32 channels, l lo; D = 64: h both of 16.
+template <int D>
+struct QueryRegs {
+  i32x8 h, l;
+  int se, sl;  // scale bytes of the 32 channels that this lane group stands for
+};
+
+// 16 channels x, scaled by 2^-e, as 4 dwords of hi and 4 of lo.
+__device__ __forceinline__ void split16(const bf16x8 (&x)[2], float inv, int* hi, int* lo) {
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    float f[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f[i] = (float)x[w / 2][w % 2 * 4 + i] * inv;
+    int h = __builtin_amdgcn_cvt_pk_fp8_f32(f[0], f[1], 0, false);
+    h = __builtin_amdgcn_cvt_pk_fp8_f32(f[2], f[3], h, true);
+    hi[w] = h;
+    f[0] = 16.f * (f[0] - __builtin_amdgcn_cvt_f32_fp8(h, 0));
+    f[1] = 16.f * (f[1] - __builtin_amdgcn_cvt_f32_fp8(h, 1));
+    f[2] = 16.f * (f[2] - __builtin_amdgcn_cvt_f32_fp8(h, 2));
+    f[3] = 16.f * (f[3] - __builtin_amdgcn_cvt_f32_fp8(h, 3));
+    int l = __builtin_amdgcn_cvt_pk_fp8_f32(f[0], f[1], 0, false);
+    lo[w] = __builtin_amdgcn_cvt_pk_fp8_f32(f[2], f[3], l, true);
+  }
+}
+
+// Scale byte of 32 channels of which x holds 16 and lane l ^ 16 the others; 255 (NaN) if
+// one is not finite.
+__device__ __forceinline__ int query_scale(const bf16x8 (&x)[2]) {
+  u16x2 top = {0, 0};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint32_t w = __builtin_bit_cast(u32x4, x[i / 4])[i % 4] & 0x7fff7fffu;
+    top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, w));
+  }
+  uint32_t m = max((uint32_t)top[0], (uint32_t)top[1]);
+  m = max(m, (uint32_t)__shfl_xor((int)m, 16));
+  if (m >= 0x7f80u) return kScaleNan;
+  return max((int)(m >> 7) - 8 + ((m & 0x7fu) > 0x60u ? 1 : 0), 8);
+}
+
+template <int D>
+__device__ __forceinline__ QueryRegs<D> load_query(const __bf16* q, bool real, int q4) {
+  QueryRegs<D> r;
+  bf16x8 x[2] = {bf16x8{}, bf16x8{}};
+  if (real) {
+    x[0] = *(const bf16x8*)(q + 16 * q4);
+    x[1] = *(const bf16x8*)(q + 16 * q4 + 8);
+  }
+  int hi[8], lo[8];
+  const int e0 = query_scale(x);  // of channels 32 (q4 / 2) ..
+  split16(x, __uint_as_float((uint32_t)(254 - e0) << 23), hi, lo);
+  if constexpr (D == 128) {
+    bf16x8 y[2] = {bf16x8{}, bf16x8{}};
+    if (real) {
+      y[0] = *(const bf16x8*)(q + 64 + 16 * q4);
+      y[1] = *(const bf16x8*)(q + 64 + 16 * q4 + 8);
+    }
+    const int e1 = query_scale(y);  // of channels 64 + 32 (q4 / 2) ..
+    split16(y, __uint_as_float((uint32_t)(254 - e1) << 23), hi + 4, lo + 4);
+    // lane group g gives the scale of channels 32 g ..: that of group 2 (g % 2)
+    const int lane = threadIdx.x & 63, from = (lane & 15) | ((q4 & 1) << 5);
+    const int s0 = __shfl(e0, from), s1 = __shfl(e1, from);
+    r.se = q4 < 2 ? s0 : s1;
+    r.sl = r.se == kScaleNan ? kScaleNan : r.se - 4;
+    r.h = i32x8{hi[0], hi[1], hi[2], hi[3], hi[4], hi[5], hi[6], hi[7]};
+    r.l = i32x8{lo[0], lo[1], lo[2], lo[3], lo[4], lo[5], lo[6], lo[7]};
+  } else {
+    // k 0 .. 63: hi, 64 .. 127: lo of the same channels
+    const int lane = threadIdx.x & 63, from = (lane & 15) | ((q4 & 1) << 5);
+    const int s0 = __shfl(e0, from);
+    r.se = q4 < 2 || s0 == kScaleNan ? s0 : s0 - 4;
+    r.h = i32x8{hi[0], hi[1], hi[2], hi[3], lo[0], lo[1], lo[2], lo[3]};
+  }
+  return r;
+}
+
+// S^T of 16 tokens: K as it is stored (a lane's 32 codes and their scale) times Q.
+template <int D>
+__device__ __forceinline__ f32x4 scores(const u32x4& k, uint32_t ks, const QueryRegs<D>& q) {
+  const i32x8 a = {(int)k[0], (int)k[1], (int)k[2], (int)k[3], 0, 0, 0, 0};
+  f32x4 c = {0.f, 0.f, 0.f, 0.f};
+  c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, q.h, c, 4, 0, 0, (int)ks, 0, q.se);
+  if constexpr (D == 128) c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, q.l, c, 4, 0, 0, (int)ks, 0, q.sl);
+  return c;
+}
+
+// What a list costs beyond its pages (page numbers, Q, the first page's latency, the joined
+// states), in pages: with 57 units a workgroup those of the shortest lists took 238,000 cycles
+// and the mean 123,000 where this was left out.
+constexpr int kListCost = 8;
+
 // How the live pages of a call are dealt to the workgroups: all lists one after
-// another in the order (sequence, key/value head, page), workgroup w takes units
-// [w U, (w + 1) U) of them.  A list that lies in more than one workgroup is joined
+// another in the order (sequence, key/value head, page), kListCost units and one for
+// every page each, and workgroup w takes units [w U, (w + 1) U) of them.  A list that lies in more than one workgroup is joined
 // from partial results; a workgroup leaves at most two of them, slot 2 w for the
 // first list it touches and 2 w + 1 for the last.
 struct SplitArgs {
@@ -141,44 +254,47 @@ struct SplitArgs {
   float* ml;      // {m, l} [2 groups][rows]
 };
 
-// Where the units of a call lie: computed by every workgroup from the lengths.
+// Where the units of a call lie, fewer than 2^31: computed by every workgroup from the
+// lengths.  All of it is the same for the whole workgroup and kept in scalar registers.
 struct Deal {
-  long long total;   // units of the call
-  long long unit;    // units per workgroup
-  int b;             // sequence asked for
-  long long before;  // units before it
+  int total;   // units of the call
+  int unit;    // units per workgroup
+  int b;       // sequence asked for
+  int before;  // units before it
 };
+
+__device__ __forceinline__ int list_units(const Span& s) { return s.count > 0 ? s.count + kListCost : 0; }
 
 // The sequence of this workgroup's first unit (seq < 0), or sequence seq.  Thread t counts
 // the sequences t per .. t per + per - 1, and the one that has the answer leaves it in LDS.
 __device__ __forceinline__ Deal make_deal(const CacheArgs& a, const SplitArgs& sa, int rows,
-                                          long long* lds, int seq) {
+                                          int* lds, int seq) {
   constexpr int T = 64 * kWaves;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int per = (a.B + T - 1) / T, b0 = tid * per, b1 = min(b0 + per, a.B);
-  long long mine = 0;
-  for (int b = b0; b < b1; ++b) mine += (long long)make_span(a, b, 0, rows).count * a.Hkv;
-  long long inc = mine;
+  int mine = 0;
+  for (int b = b0; b < b1; ++b) mine += list_units(make_span(a, b, 0, rows)) * a.Hkv;
+  int inc = mine;
 #pragma unroll
   for (int o = 1; o < 64; o *= 2) {
-    const long long y = __shfl_up(inc, o);
+    const int y = __shfl_up(inc, o);
     if (lane >= o) inc += y;
   }
   if (lane == 63) lds[wave] = inc;
   __syncthreads();
-  long long before = inc - mine, total = 0;
+  int before = inc - mine, total = 0;
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) {
     before += w < wave ? lds[w] : 0;
     total += lds[w];
   }
   Deal d;
-  d.total = total;
-  d.unit = max((long long)sa.least, (total + sa.groups - 1) / sa.groups);
+  d.total = __builtin_amdgcn_readfirstlane(total);
+  d.unit = max(sa.least, (d.total + sa.groups - 1) / sa.groups);
   const long long want = (long long)blockIdx.x * d.unit;
   if (seq < 0 ? want >= before && want < before + mine : seq >= b0 && seq < b1) {
     for (int b = b0; b < b1; ++b) {
-      const long long n = (long long)make_span(a, b, 0, rows).count * a.Hkv;
+      const int n = list_units(make_span(a, b, 0, rows)) * a.Hkv;
       if (seq < 0 ? want < before + n : b == seq) {
         lds[kWaves] = b;
         lds[kWaves + 1] = before;
@@ -188,8 +304,9 @@ __device__ __forceinline__ Deal make_deal(const CacheArgs& a, const SplitArgs& s
     }
   }
   __syncthreads();
-  d.b = (int)lds[kWaves];
-  d.before = lds[kWaves + 1];
+  d.b = __builtin_amdgcn_readfirstlane(lds[kWaves]);
+  d.before = __builtin_amdgcn_readfirstlane(lds[kWaves + 1]);
+  __syncthreads();
   return d;
 }
 
@@ -228,16 +345,14 @@ __device__ __forceinline__ void store_row(const CacheArgs& a, const Span& sp, in
 // waves take every fourth page of a list, each with a state of its own, joined at
 // the list's (or the workgroup's) end.
 template <int D, int NT>
-__global__ __launch_bounds__(64 * kWaves, NT == 1 ? 3 : NT == 2 ? 2 : 1) void k_cache_token(CacheArgs a, SplitArgs sa) {
+__global__ __launch_bounds__(64 * kWaves, waves_per_simd(D, NT)) void k_cache_token(CacheArgs a, SplitArgs sa) {
   using R = Record<D>;
-  using Regs = PageRegs<D>;
-  using Codes = typename Regs::Codes;
-  constexpr int KW = D / 32;        // dwords of codes per lane and 16 tokens, K steps of 32 channels
   constexpr int GR = D / 32;        // scale groups
   constexpr int CT = D / 16;        // channel tiles of the output
   constexpr int VROW = D / 2;       // bytes of a token's V codes
   constexpr int OP = D + 4;         // padded output row in LDS
-  constexpr int kWaveBytes = 64 * VROW + 2 * 64 * GR * 4;
+  constexpr int kVBytes = 64 * VROW;
+  constexpr int kWaveBytes = 2 * kVBytes + 64 * GR * 2;
   constexpr int kJoinBytes = kWaves * 16 * (OP + 2) * 4;
   constexpr int kLds = kWaves * kWaveBytes > kJoinBytes ? kWaves * kWaveBytes : kJoinBytes;
   __shared__ __attribute__((aligned(16))) char lds[kLds];
@@ -246,8 +361,8 @@ __global__ __launch_bounds__(64 * kWaves, NT == 1 ? 3 : NT == 2 ? 2 : 1) void k_
   const int n = lane & 15, q4 = lane >> 4;
   const int rows = a.S_q * a.G;
 
-  long long left;        // units of this workgroup
-  int b, g, off;         // list and page of the next one
+  int left;              // units of this workgroup
+  int b, g, off;         // list and unit of it of the next one
   bool split;
   if (sa.part == nullptr) {
     b = blockIdx.x / a.Hkv;
@@ -256,17 +371,15 @@ __global__ __launch_bounds__(64 * kWaves, NT == 1 ? 3 : NT == 2 ? 2 : 1) void k_
     left = 1;  // one list, whatever its length
     split = false;
   } else {
-    const Deal d = make_deal(a, sa, rows, (long long*)lds, -1);
-    __syncthreads();
+    const Deal d = make_deal(a, sa, rows, (int*)lds, -1);
     const long long lo = (long long)blockIdx.x * d.unit;
-    left = min(d.unit, d.total - lo);
+    left = (int)max(min((long long)d.unit, d.total - lo), 0ll);
+    b = g = off = 0;
     if (left > 0) {
-      const int count = make_span(a, d.b, 0, rows).count;
+      const int n = list_units(make_span(a, d.b, 0, rows)), at = (int)lo - d.before;
       b = d.b;
-      g = (int)((lo - d.before) / count);
-      off = (int)(lo - d.before - (long long)g * count);
-    } else {
-      b = g = off = 0;
+      g = __builtin_amdgcn_readfirstlane(at / n);
+      off = at - g * n;
     }
     split = true;
     // lists without a page: their rows are zero
@@ -279,30 +392,25 @@ __global__ __launch_bounds__(64 * kWaves, NT == 1 ? 3 : NT == 2 ? 2 : 1) void k_
     }
   }
 
-  char* wv = lds + wave * kWaveBytes;         // V codes, swizzled
-  float* wks = (float*)(wv + 64 * VROW);      // K scales [group][token]
-  float* wvs = wks + 64 * GR;                 // V scales [group][token]
+  char* wv = lds + wave * kWaveBytes;  // V codes of two pages, 16-byte chunks swizzled in their rows
+  unsigned short* wvs = (unsigned short*)(wv + 2 * kVBytes);  // V scales [group][token] as bf16
+  const uint32_t wv_lds = lds_addr(wv);
 
   bool first = true;
   for (; left > 0; first = false) {
     const Span sp = make_span(a, b, 0, rows);
-    const int end = split ? (int)min((long long)sp.count, off + left) : sp.count;
+    const int units = list_units(sp), last = split ? min(units, off + left) : units;
+    const int begin = max(off - kListCost, 0), end = max(last - kListCost, 0);
 
     // this lane's query rows, and its part of Q as the B operand
-    bf16x8 qf[NT][KW];
+    QueryRegs<D> qf[NT];
     int pos[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
       const int row = 16 * t + n, qi = row / a.G;
       const bool real = row < rows && qi < sp.n;
       pos[t] = real ? sp.first + qi : -1;
-#pragma unroll
-      for (int s = 0; s < KW; ++s) qf[t][s] = bf16x8{};
-      if (real) {
-        const __bf16* qp = a.q + b * a.q_sb + (g * a.G + row % a.G) * a.q_sh + qi * a.q_ss + q4 * (D / 4);
-#pragma unroll
-        for (int s = 0; s < KW; ++s) qf[t][s] = *(const bf16x8*)(qp + 8 * s);
-      }
+      qf[t] = load_query<D>(a.q + b * a.q_sb + (g * a.G + row % a.G) * a.q_sh + qi * a.q_ss, real, q4);
     }
 
     f32x4 o[NT][CT];
@@ -316,7 +424,7 @@ __global__ __launch_bounds__(64 * kWaves, NT == 1 ? 3 : NT == 2 ? 2 : 1) void k_
     }
 
     // page numbers of this wave's next 64 pages, one per lane; -1: no key of it is visible
-    int ids = -1, base = off + wave;
+    int ids = -1, base = begin + wave;
     auto load_ids = [&](int from) {
       const int i = from + kWaves * lane;
       int id = -1;
@@ -329,90 +437,72 @@ __global__ __launch_bounds__(64 * kWaves, NT == 1 ? 3 : NT == 2 ? 2 : 1) void k_
       return id;
     };
     auto record = [&](int id) { return a.pages + ((size_t)id * a.Hkv + g) * R::kBytes; };
-    Regs x;
+    // a lane's places in a record.  K, D = 64: lane groups 2 and 3 hold the channels of 0
+    // and 1 again
+    const uint32_t grp = GR == 4 ? q4 : q4 & 1;
+    const uint32_t k_at = n * R::kRow + grp * 16, ks_at = R::kKs + n * GR + grp;
+    const uint32_t vs_at = R::kVs + GR * lane;
+    PageRegs x;
     auto load_k = [&](const uint8_t* rec) {
-      const uint8_t* at = rec + n * R::kRow + q4 * 4 * KW;
-      x.k0 = *(const Codes*)at;
-      x.k1 = *(const Codes*)(at + 16 * R::kRow);
-      x.k2 = *(const Codes*)(at + 32 * R::kRow);
-      x.k3 = *(const Codes*)(at + 48 * R::kRow);
+      x.k0 = *(const u32x4*)(rec + k_at);
+      x.k1 = *(const u32x4*)(rec + 16 * R::kRow + k_at);
+      x.k2 = *(const u32x4*)(rec + 32 * R::kRow + k_at);
+      x.k3 = *(const u32x4*)(rec + 48 * R::kRow + k_at);
+      x.ks0 = (rec + ks_at)[0];
+      x.ks1 = (rec + 16 * GR + ks_at)[0];
+      x.ks2 = (rec + 32 * GR + ks_at)[0];
+      x.ks3 = (rec + 48 * GR + ks_at)[0];
+      if constexpr (GR == 4) x.vs = *(const uint32_t*)(rec + vs_at);
+      else x.vs = *(const unsigned short*)(rec + vs_at);
     };
-    auto load_v = [&](const uint8_t* rec) {
-      const uint8_t* at = rec + R::kV + n * R::kRow + q4 * 4 * KW;
-      if constexpr (GR == 4) {
-        x.ks = *(const uint32_t*)(rec + R::kKs + 4 * lane);
-        x.vs = *(const uint32_t*)(rec + R::kVs + 4 * lane);
-      } else {
-        x.ks = *(const unsigned short*)(rec + R::kKs + 2 * lane);
-        x.vs = *(const unsigned short*)(rec + R::kVs + 2 * lane);
-      }
-      x.v0 = *(const Codes*)at;
-      x.v1 = *(const Codes*)(at + 16 * R::kRow);
-      x.v2 = *(const Codes*)(at + 32 * R::kRow);
-      x.v3 = *(const Codes*)(at + 48 * R::kRow);
+    // V codes straight to LDS: chunk c of token row r at slot c ^ (r / 4) % 4 (D = 128, 4
+    // chunks a row) or c ^ (r / 8) % 2 (D = 64, 2 chunks)
+    constexpr int CPR = VROW / 16, RPC = 64 / CPR;  // chunks per row, rows per copy
+    const uint32_t v_chunk = (lane % CPR) ^ (D == 128 ? (lane >> 4) & 3 : (lane >> 4) & 1);
+    const uint32_t v_at = R::kV + lane / CPR * VROW + v_chunk * 16;
+    auto copy_v = [&](const uint8_t* rec, int buf) {
+#pragma unroll
+      for (int j = 0; j < 64 / RPC; ++j)
+        copy16_to_lds(rec + j * 1024, v_at, wv_lds + buf * kVBytes + j * 1024);
     };
 
-    int id = -1;
+    int id = -1, buf = 0;
     if (base < end) {
       ids = load_ids(base);
       id = __builtin_amdgcn_readfirstlane(ids);
-      load_v(record(max(id, 0)));
+      copy_v(record(max(id, 0)), 0);
       load_k(record(max(id, 0)));
     }
-    for (int i = base; i < end; i += kWaves) {
+    for (int i = base; i < end; i += kWaves, buf ^= 1) {
       const bool there = id >= 0;  // else page 0 stands in, none of its keys visible
-      // V and the scales to LDS
-      {
-        auto at = [&](int t) {  // 16 (D = 128) or 8 bytes, swizzled within the token's row
-          const int slot = D == 128 ? (q4 ^ (n >> 2)) * 16 : (q4 ^ ((n >> 3) | ((t & 1) << 1))) * 8;
-          return (Codes*)(wv + (16 * t + n) * VROW + slot);
-        };
-        *at(0) = x.v0;
-        *at(1) = x.v1;
-        *at(2) = x.v2;
-        *at(3) = x.v3;
-      }
-      // all scale bytes of a vector are 255, or none: tokens that stand for NaN
-      const uint64_t k_nan = __builtin_amdgcn_ballot_w64((x.ks & 0xff) == kScaleNan);
-      const uint64_t v_nan = __builtin_amdgcn_ballot_w64((x.vs & 0xff) == kScaleNan);
-      const uint32_t vs = (x.vs & 0xff) == kScaleNan ? 0x7f7f7f7fu : x.vs;
-#pragma unroll
-      for (int gr = 0; gr < GR; ++gr) {
-        wks[64 * gr + lane] = __uint_as_float(((x.ks >> (8 * gr)) & 0xff) << 23);
-        wvs[64 * gr + lane] = __uint_as_float(((vs >> (8 * gr)) & 0xff) << 23);
-      }
-      // the next page on its way: V and scales here, K behind its last use
-      const int k = (i + kWaves - base) / kWaves;
-      if (i + kWaves < end) {
-        if (k % 64 == 0) ids = load_ids(i + kWaves);
-        id = __builtin_amdgcn_readlane(ids, k % 64);
-      }
-      const uint8_t* next = record(max(id, 0));
-      load_v(next);
-
       // S^T: 4 tiles of 16 tokens
       f32x4 sc[NT][4];
 #pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        __builtin_amdgcn_sched_barrier(0);
-        const float ksc = wks[64 * (q4 * GR / 4) + 16 * t + n];
-#pragma unroll
-        for (int s = 0; s < KW; ++s) {
-          const bf16x8 kf = decode8((t == 0 ? x.k0 : t == 1 ? x.k1 : t == 2 ? x.k2 : x.k3)[s], ksc);
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
-            sc[nt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                kf, qf[nt][s], s == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : sc[nt][t], 0, 0, 0);
-        }
+      for (int nt = 0; nt < NT; ++nt) {
+        sc[nt][0] = scores<D>(x.k0, x.ks0, qf[nt]);
+        sc[nt][1] = scores<D>(x.k1, x.ks1, qf[nt]);
+        sc[nt][2] = scores<D>(x.k2, x.ks2, qf[nt]);
+        sc[nt][3] = scores<D>(x.k3, x.ks3, qf[nt]);
       }
-      load_k(next);
-      if (k_nan != 0)
-        for_tokens(k_nan, q4, [&](int e, bool in) {
+      // all scale bytes of a vector are 255, or none: tokens that stand for NaN
+      const uint64_t v_nan = __builtin_amdgcn_ballot_w64((x.vs & 0xff) == kScaleNan);
+      const bool v_large = __builtin_amdgcn_ballot_w64((x.vs & (x.vs << 1) & 0x80808080u) != 0) != 0;
+      const uint32_t vs = (x.vs & 0xff) == kScaleNan ? 0x7f7f7f7fu : x.vs;
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt) sc[nt][e / 4][e % 4] = in ? NAN : sc[nt][e / 4][e % 4];
-        });
+      for (int gr = 0; gr < GR; ++gr)
+        wvs[64 * gr + lane] = (unsigned short)((vs >> (8 * gr) & 0xff) << 7);
+      wait_vm<0>();  // this page's V is in LDS (and its K was used)
+      // the next page on its way
+      if (i + kWaves < end) {
+        const int k = (i + kWaves - base) / kWaves;
+        if (k % 64 == 0) ids = load_ids(i + kWaves);
+        id = __builtin_amdgcn_readlane(ids, k % 64);
+        copy_v(record(max(id, 0)), buf ^ 1);
+        load_k(record(max(id, 0)));
+      }
       const int kb = span_page(sp, i);
-      if (!there || !page_full(a, sp, kb)) {
+      const bool full = there && page_full(a, sp, kb);
+      if (!full) {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
           const int lim = there ? row_limit(a, sp, pos[nt], kb) - 4 * q4 : -1;
@@ -447,6 +537,7 @@ __global__ __launch_bounds__(64 * kWaves, NT == 1 ? 3 : NT == 2 ? 2 : 1) void k_
           for (int c = 0; c < CT; ++c) o[nt][c] *= alpha;
         }
       }
+      // P = 2^(S c - m) in bf16, two to a register
       uint32_t poison[NT];  // this lane's weights of values that stand for NaN, seen by their rows
       if (v_nan != 0) {
 #pragma unroll
@@ -457,55 +548,89 @@ __global__ __launch_bounds__(64 * kWaves, NT == 1 ? 3 : NT == 2 ? 2 : 1) void k_
             poison[nt] |= in && sc[nt][e / 4][e % 4] != -INFINITY ? 1u << e : 0u;
         });
       }
-      float p[NT][16];
+      uint32_t pk[NT][8];
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          p[nt][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[nt][e / 4][e % 4], a.c, -ms[nt]));
-          l[nt] += p[nt][e];
+        for (int e = 0; e < 8; ++e) {
+          const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[nt][e / 2][e % 2 * 2], a.c, -ms[nt]));
+          const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[nt][e / 2][e % 2 * 2 + 1], a.c, -ms[nt]));
+          l[nt] += p0;
+          l[nt] += p1;
+          pk[nt][e] = pack_bf16(p0, p1);
         }
       if (v_nan != 0) {
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          asm volatile("" : "+v"(poison[nt]));
+        for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-          for (int e = 0; e < 16; ++e) p[nt][e] = poison[nt] >> e & 1 ? NAN : p[nt][e];
-        }
+          for (int e = 0; e < 8; ++e) {
+            if (poison[nt] >> (2 * e) & 1) pk[nt][e] = (pk[nt][e] & 0xffff0000u) | 0x7fc0u;
+            if (poison[nt] >> (2 * e + 1) & 1) pk[nt][e] = (pk[nt][e] & 0xffffu) | 0x7fc00000u;
+          }
       }
-      // O^T += V^T P^T, 32 channels (one scale per token) at a time
+      // O^T += V^T P^T, 32 channels (one scale per token) at a time.  The scaling of P is an
+      // addition to both exponents of a pair: P + (e - 127) in units of 2^7, not below 0.  A
+      // weight under 2^-126 then ends as up to 2^(e - 254), 2^-127 of what the token's values
+      // can be, which is nothing where the row sees the token; where it may not, and where
+      // e > 191 might carry into the sign, zero weights stay 0 and the sum is kept below it.
+      const bool special = !full || v_large;
+      const char* wvb = wv + buf * kVBytes;
+      const int tok = 16 * (n >> 2) + 4 * q4 + (n & 3);
+      auto read_v = [&](int ct) {
+        const int slot = ((ct >> 1) ^ (D == 128 ? q4 : q4 >> 1)) * 16 + (ct & 1) * 8;
+        return __builtin_amdgcn_ds_read_tr4_b64_v2i32((lds_i32x2*)(wvb + tok * VROW + slot));
+      };
+      // the next 32 channels' operands are read ahead of the present ones' use, and no further
+      u32x2 sv[2][4];
+      i32x2 w[2][2];
+      auto read_group = [&](int gr) {
+#pragma unroll
+        for (int t = 0; t < 4; ++t) sv[gr & 1][t] = *(const u32x2*)(wvs + 64 * gr + 16 * t + 4 * q4);
+        w[gr & 1][0] = read_v(2 * gr);
+        w[gr & 1][1] = read_v(2 * gr + 1);
+      };
+      read_group(0);
 #pragma unroll
       for (int gr = 0; gr < GR; ++gr) {
-        __builtin_amdgcn_sched_barrier(0);  // else all groups' operands are held at one time
-        f32x4 sv[4];
-#pragma unroll
-        for (int t = 0; t < 4; ++t) sv[t] = *(const f32x4*)(wvs + 64 * gr + 16 * t + 4 * q4);
-        bf16x8 pf[NT][2];
+        __builtin_amdgcn_sched_barrier(0);
+        if (gr + 1 < GR) read_group(gr + 1);
+        u32x4 u[NT][2];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-          for (int e = 0; e < 16; ++e)
-            pf[nt][e / 8][e % 8] = (__bf16)(p[nt][e] * sv[e / 4][e % 4]);
+          for (int e = 0; e < 8; ++e) {
+            const uint32_t se = sv[gr & 1][e / 2][e % 2];
+            const u16x2 y = __builtin_bit_cast(u16x2, pk[nt][e]) + __builtin_bit_cast(u16x2, se);
+            u[nt][e / 4][e % 4] = __builtin_bit_cast(uint32_t, __builtin_elementwise_sub_sat(y, u16x2{0x3f80, 0x3f80}));
+          }
+        if (special) {
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const uint32_t ue = u[nt][e / 4][e % 4];
+              const u16x2 some = __builtin_elementwise_min(__builtin_bit_cast(u16x2, pk[nt][e]), u16x2{1, 1});
+              const u16x2 y = __builtin_elementwise_min(__builtin_bit_cast(u16x2, ue), u16x2{0x7fc0, 0x7fc0});
+              u[nt][e / 4][e % 4] = __builtin_bit_cast(uint32_t, some * y);
+            }
+        }
 #pragma unroll
         for (int c2 = 0; c2 < 2; ++c2) {
           const int ct = 2 * gr + c2;
-          const int tok = 16 * (n >> 2) + 4 * q4 + (n & 3);
-          const int slot = D == 128 ? ((ct >> 1) ^ q4) * 16 + (ct & 1) * 8
-                                    : (ct ^ ((q4 >> 1) | (((n >> 2) & 1) << 1))) * 8;
-          const i32x2 w = __builtin_amdgcn_ds_read_tr4_b64_v2i32((lds_i32x2*)(wv + tok * VROW + slot));
-          const bf16x8 v0 = decode8((uint32_t)w[0], 1.f), v1 = decode8((uint32_t)w[1], 1.f);
+          const bf16x8 v0 = decode8((uint32_t)w[gr & 1][c2][0], 1.f), v1 = decode8((uint32_t)w[gr & 1][c2][1], 1.f);
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) {
-            o[nt][ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, pf[nt][0], o[nt][ct], 0, 0, 0);
-            o[nt][ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, pf[nt][1], o[nt][ct], 0, 0, 0);
+            o[nt][ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, __builtin_bit_cast(bf16x8, u[nt][0]), o[nt][ct], 0, 0, 0);
+            o[nt][ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, __builtin_bit_cast(bf16x8, u[nt][1]), o[nt][ct], 0, 0, 0);
           }
         }
       }
     }
 
     // the waves' states of a row joined, then the rows or a partial result stored
-    const bool whole = off == 0 && end == sp.count;
+    const bool whole = off == 0 && last == units;
     const size_t slot = 2 * (size_t)blockIdx.x + (first ? 0 : 1);
+    const int tid = thread_here(), en = tid & 15, eq4 = tid >> 4 & 3, ew = tid >> 6;
     float* jo = (float*)lds;              // [wave][16][OP]
     float* jml = jo + kWaves * 16 * OP;   // [wave][16][2]
 #pragma unroll
@@ -513,15 +638,15 @@ __global__ __launch_bounds__(64 * kWaves, NT == 1 ? 3 : NT == 2 ? 2 : 1) void k_
       __syncthreads();
       const float ls = row_sum(l[nt]);
 #pragma unroll
-      for (int c = 0; c < CT; ++c) *(f32x4*)(jo + (wave * 16 + n) * OP + 16 * c + 4 * q4) = o[nt][c];
-      if (q4 == 0) {
-        jml[(wave * 16 + n) * 2] = m[nt];
-        jml[(wave * 16 + n) * 2 + 1] = ls;
+      for (int c = 0; c < CT; ++c) *(f32x4*)(jo + (ew * 16 + en) * OP + 16 * c + 4 * eq4) = o[nt][c];
+      if (eq4 == 0) {
+        jml[(ew * 16 + en) * 2] = m[nt];
+        jml[(ew * 16 + en) * 2 + 1] = ls;
       }
       __syncthreads();
       constexpr int TPR = 64 * kWaves / 16;     // threads per row
       constexpr int EPT = D / TPR;              // elements per thread
-      const int jr = threadIdx.x / TPR, d0 = threadIdx.x % TPR * EPT, r = 16 * nt + jr;
+      const int jr = tid / TPR, d0 = tid % TPR * EPT, r = 16 * nt + jr;
       if (r < rows) {
         float top = -INFINITY;
 #pragma unroll
@@ -553,7 +678,7 @@ __global__ __launch_bounds__(64 * kWaves, NT == 1 ? 3 : NT == 2 ? 2 : 1) void k_
     __syncthreads();
 
     if (!split) break;
-    left -= end - off;
+    left -= last - off;
     off = 0;
     if (++g == a.Hkv) {
       g = 0;
@@ -575,10 +700,9 @@ __global__ __launch_bounds__(64 * kWaves) void k_cache_join(CacheArgs a, SplitAr
   const int rows = a.S_q * a.G, b = blockIdx.x / a.Hkv, g = blockIdx.x % a.Hkv, r = blockIdx.y;
   const Span sp = make_span(a, b, 0, rows);
   if (sp.count == 0) return;  // uniform over the workgroup
-  const Deal d = make_deal(a, sa, rows, (long long*)lds, b);
-  __syncthreads();
-  const long long lo = d.before + (long long)g * sp.count;
-  const int w0 = (int)(lo / d.unit), w1 = (int)((lo + sp.count - 1) / d.unit);
+  const Deal d = make_deal(a, sa, rows, (int*)lds, b);
+  const int units = list_units(sp), lo = d.before + g * units;
+  const int w0 = lo / d.unit, w1 = (lo + units - 1) / d.unit;
   if (w0 == w1) return;  // stored by its workgroup
   const int first = 2 * w0 + (lo == w0 * d.unit ? 0 : 1);
   const int c = threadIdx.x % C, pg = threadIdx.x / C;
@@ -827,7 +951,7 @@ TokenPlan token_plan(int B, int Hkv, int rows, int D, int M) {
   TokenPlan p{};
   const long long lists = (long long)B * Hkv, most = lists * M;
   const long long want = (most + 3) / 4;
-  const int most_groups = 256 * (rows <= 16 ? 3 : rows <= 32 ? 2 : 1);
+  const int most_groups = 256 * waves_per_simd(D, rows <= 16 ? 1 : 2);
   p.groups = (int)(want < most_groups ? want : most_groups);
   p.split = M > 16;
   if (!p.split) p.groups = (int)lists;
@@ -842,19 +966,18 @@ template <int D>
 void launch_token(const CacheArgs& a, const SplitArgs& sa, int groups, int rows, hipStream_t s) {
   const dim3 grid(groups), wg(64 * kWaves);
   if (rows <= 16) hipLaunchKernelGGL((k_cache_token<D, 1>), grid, wg, 0, s, a, sa);
-  else if (rows <= 32) hipLaunchKernelGGL((k_cache_token<D, 2>), grid, wg, 0, s, a, sa);
-  else hipLaunchKernelGGL((k_cache_token<D, 4>), grid, wg, 0, s, a, sa);
+  else hipLaunchKernelGGL((k_cache_token<D, 2>), grid, wg, 0, s, a, sa);
   if (sa.part != nullptr) hipLaunchKernelGGL(k_cache_join<D>, dim3(a.B * a.Hkv, rows), wg, 0, s, a, sa);
 }
 
 size_t cache_attn_ws(int B, int Hq, int Hkv, int S_q, int D, int M) {
   const int rows = S_q * (Hq / Hkv);
-  return rows <= 64 ? token_plan(B, Hkv, rows, D, M).total : 256;
+  return rows <= 32 ? token_plan(B, Hkv, rows, D, M).total : 256;
 }
 
 hipError_t launch_cache_attn(const CacheArgs& a, int D, void* ws, hipStream_t s) {
   const int rows = a.S_q * a.G;
-  if (rows <= 64) {
+  if (rows <= 32) {
     const TokenPlan p = token_plan(a.B, a.Hkv, rows, D, a.M);
     SplitArgs sa{};
     sa.groups = p.groups;

@@ -344,6 +344,8 @@ int check_cache_heads(int B, int Hq, int Hkv, int S_q, int D, int max_pages, int
     return fail(STEEL_ERR_INVALID_ARGUMENT, "Hq (%d) must be a multiple of Hkv (%d)", Hq, Hkv);
   if ((long long)B * Hq * S_q > INT32_MAX / 2)
     return fail(STEEL_ERR_UNSUPPORTED, "B * Hq * S_q = %d * %d * %d rows are too many", B, Hq, S_q);
+  if ((long long)B * Hkv * max_pages > INT32_MAX / 2)
+    return fail(STEEL_ERR_UNSUPPORTED, "B * Hkv * max_pages = %d * %d * %d is too large", B, Hkv, max_pages);
   return STEEL_OK;
 }
 
