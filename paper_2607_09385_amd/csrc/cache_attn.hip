@@ -176,8 +176,9 @@ __device__ __forceinline__ void split16(const bf16x8 (&x)[2], float inv, int* hi
   }
 }
 
-// Scale byte of 32 channels of which x holds 16 and lane l ^ 16 the others; 255 (NaN) if
+// Scale byte of 32 channels of which x holds 16 and lane l ^ OTHER the others; 255 (NaN) if
 // one is not finite.
+template <int OTHER>
 __device__ __forceinline__ int query_scale(const bf16x8 (&x)[2]) {
   u16x2 top = {0, 0};
 #pragma unroll
@@ -186,7 +187,7 @@ __device__ __forceinline__ int query_scale(const bf16x8 (&x)[2]) {
     top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, w));
   }
   uint32_t m = max((uint32_t)top[0], (uint32_t)top[1]);
-  m = max(m, (uint32_t)__shfl_xor((int)m, 16));
+  m = max(m, (uint32_t)__shfl_xor((int)m, OTHER));
   if (m >= 0x7f80u) return kScaleNan;
   return max((int)(m >> 7) - 8 + ((m & 0x7fu) > 0x60u ? 1 : 0), 8);
 }
@@ -200,7 +201,7 @@ __device__ __forceinline__ QueryRegs<D> load_query(const __bf16* q, bool real, i
     x[1] = *(const bf16x8*)(q + 16 * q4 + 8);
   }
   int hi[8], lo[8];
-  const int e0 = query_scale(x);  // of channels 32 (q4 / 2) ..
+  const int e0 = query_scale<16>(x);  // of channels 32 (q4 / 2) ..
   split16(x, __uint_as_float((uint32_t)(254 - e0) << 23), hi, lo);
   if constexpr (D == 128) {
     bf16x8 y[2] = {bf16x8{}, bf16x8{}};
@@ -208,7 +209,7 @@ __device__ __forceinline__ QueryRegs<D> load_query(const __bf16* q, bool real, i
       y[0] = *(const bf16x8*)(q + 64 + 16 * q4);
       y[1] = *(const bf16x8*)(q + 64 + 16 * q4 + 8);
     }
-    const int e1 = query_scale(y);  // of channels 64 + 32 (q4 / 2) ..
+    const int e1 = query_scale<16>(y);  // of channels 64 + 32 (q4 / 2) ..
     split16(y, __uint_as_float((uint32_t)(254 - e1) << 23), hi + 4, lo + 4);
     // lane group g gives the scale of channels 32 g ..: that of group 2 (g % 2)
     const int lane = threadIdx.x & 63, from = (lane & 15) | ((q4 & 1) << 5);
@@ -736,208 +737,357 @@ __global__ __launch_bounds__(64 * kWaves) void k_cache_join(CacheArgs a, SplitAr
   store_row<4>(a, sp, D, b, g, r, 4 * c, out, ms, l);
 }
 
-constexpr int kRows = 16;
-template <int D>
-struct TileRegs {
-  static constexpr int KW = D / 32;
-  uint32_t k[4][KW], v[4][KW], ks, vs;
+// Many rows per key/value head (chunks of prompts): tiles of 128 rows, 4 waves of 32.
+//
+// S^T = K Q^T and O^T = V^T P^T on 32x32 MFMAs, a row in the lanes l % 32.  A page's K codes go
+// to LDS as they are and into scaled MFMAs; its V is turned into bf16 by the whole
+// workgroup (16 conversions and four 16-byte LDS writes a thread) and read
+// transposed, as the dense kernels do.  Both are one page ahead: K by copies, V's codes in
+// registers until the present page is done.
+struct ChunkArgs {
+  int tiles, ns;  // tiles of a (sequence, key/value head), segments of a tile's list
+  float* part;    // O [unit][tile][ns][128][D] when ns > 1
+  float* ml;      // {m, l}
 };
 
+constexpr int kTile = 128;
 
-// One workgroup per (sequence, key/value head, 16 rows); its waves take every
-// fourth live page, each with a state of its own, joined at the end.
+// Workgroup -> (unit, tile, segment).  With a multiple of 8 units each keeps to one XCD,
+// whose L2 then holds its keys and values; a unit's heaviest tiles come first.
+__device__ __forceinline__ void chunk_item(const CacheArgs& a, const ChunkArgs& ca, int* unit, int* tile,
+                                           int* seg) {
+  const int per = ca.tiles * ca.ns, units = a.B * a.Hkv, i = blockIdx.x;
+  int at = i;
+  if (units % 8 == 0) {
+    const int x = i & 7, j = i >> 3;
+    *unit = j / per * 8 + x;
+    at = j % per;
+  } else {
+    *unit = i / per;
+    at = i % per;
+  }
+  *tile = ca.tiles - 1 - at / ca.ns;
+  *seg = at % ca.ns;
+}
+
 template <int D>
-__global__ __launch_bounds__(64 * kWaves) void k_cache_attn(CacheArgs a, int tiles) {
+__global__ __launch_bounds__(256, 2) void k_cache_chunk(CacheArgs a, ChunkArgs ca) {
   using R = Record<D>;
-  using Regs = TileRegs<D>;
-  constexpr int KW = Regs::KW;      // also: K steps of 32 channels
-  constexpr int GR = D / 32;        // scale groups
-  constexpr int CT = D / 16;        // channel tiles of the output
-  constexpr int VROW = D / 2;       // bytes of a token's V codes
-  constexpr int OP = D + 4;         // padded output row in LDS
-  constexpr int kWaveBytes = 64 * VROW + 64 * GR * 2;
-  constexpr int kJoinBytes = kWaves * kRows * (OP + 2) * 4;
-  constexpr int kLds = kWaves * kWaveBytes > kJoinBytes ? kWaves * kWaveBytes : kJoinBytes;
-  __shared__ __attribute__((aligned(16))) char lds[kLds];
+  constexpr int KS = D / 64;        // K steps of 64 channels
+  constexpr int GR = D / 32, DT = D / 32;
+  constexpr int VROW = D / 2;       // bytes of a token's codes
+  constexpr int RB = 2 * D;         // bytes of a token's values in bf16
+  constexpr int VB = 64 * RB, KB = 64 * VROW;
+  constexpr int CPR = VROW / 16;    // 16-byte chunks of a token's codes
+  __shared__ __attribute__((aligned(1024))) char lds[2 * VB + 2 * KB];
 
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int n = lane & 15, q4 = lane >> 4;
-  const int tile = blockIdx.x % tiles, bg = blockIdx.x / tiles;
-  const int g = bg % a.Hkv, b = bg / a.Hkv;
-  const int r0 = tile * kRows, r1 = min(r0 + kRows, a.S_q * a.G);
+  int unit, tile, seg;
+  chunk_item(a, ca, &unit, &tile, &seg);
+  const int g = unit % a.Hkv, b = unit / a.Hkv, rows = a.S_q * a.G;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n = lane & 31, hf = lane >> 5;
+  const int r0 = tile * kTile, r1 = min(r0 + kTile, rows);
   const Span sp = make_span(a, b, r0, r1);
+  const int p0 = (int)((long long)sp.count * seg / ca.ns), p1 = (int)((long long)sp.count * (seg + 1) / ca.ns);
 
-  // this lane's query row, and its part of Q as the B operand
-  const int row = r0 + n, qi = row / a.G, h = g * a.G + row % a.G;
+  // this lane's row
+  const int row = r0 + 32 * wave + n, qi = row / a.G;
   const bool real = row < r1 && qi < sp.n;
   const int pos = real ? sp.first + qi : -1;
-  bf16x8 qf[KW];
+  i32x8 qh[KS], ql[KS];
+  int se[KS], sl[KS];  // scale bytes: lane half h gives those of channels 64 s + 32 h ..
+  {
+    const __bf16* q = a.q + b * a.q_sb + (g * a.G + row % a.G) * a.q_sh + qi * a.q_ss + 16 * hf;
 #pragma unroll
-  for (int s = 0; s < KW; ++s) qf[s] = bf16x8{};
-  if (real) {
-    const __bf16* qp = a.q + b * a.q_sb + h * a.q_sh + qi * a.q_ss + q4 * (D / 4);
+    for (int s = 0; s < KS; ++s) {
+      int hi[8], lo[8], e[2];
 #pragma unroll
-    for (int s = 0; s < KW; ++s) qf[s] = *(const bf16x8*)(qp + 8 * s);
-  }
-
-  char* wv = lds + wave * kWaveBytes;        // V codes, then K scales, V scales
-  char* wks = wv + 64 * VROW;
-  char* wvs = wks + 64 * GR;
-
-  f32x4 o[CT];
-#pragma unroll
-  for (int c = 0; c < CT; ++c) o[c] = f32x4{0.f, 0.f, 0.f, 0.f};
-  float m = -INFINITY, l = 0.f;
-
-  for (int i = wave; i < sp.count; i += kWaves) {
-    const int kb = span_page(sp, i);
-    const int id = a.table[(size_t)b * a.M + kb];
-    if (id < 0 || id >= a.n_pages) continue;
-    if (a.mask != nullptr && a.mask[((size_t)b * a.Hkv + g) * a.M + kb] == 0) continue;
-    const uint8_t* rec = a.pages + ((size_t)id * a.Hkv + g) * R::kBytes;
-    Regs x;
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      __builtin_memcpy(x.k[t], rec + (16 * t + n) * R::kRow + q4 * 4 * KW, 4 * KW);
-      __builtin_memcpy(x.v[t], rec + R::kV + (16 * t + n) * R::kRow + q4 * 4 * KW, 4 * KW);
-    }
-    if constexpr (GR == 4) {
-      x.ks = *(const uint32_t*)(rec + R::kKs + 4 * lane);
-      x.vs = *(const uint32_t*)(rec + R::kVs + 4 * lane);
-      *(uint32_t*)(wks + 4 * lane) = x.ks;
-      *(uint32_t*)(wvs + 4 * lane) = x.vs;
-    } else {
-      x.ks = *(const unsigned short*)(rec + R::kKs + 2 * lane);
-      x.vs = *(const unsigned short*)(rec + R::kVs + 2 * lane);
-      *(unsigned short*)(wks + 2 * lane) = (unsigned short)x.ks;
-      *(unsigned short*)(wvs + 2 * lane) = (unsigned short)x.vs;
-    }
-#pragma unroll
-    for (int t = 0; t < 4; ++t)
-      __builtin_memcpy(wv + (16 * t + n) * VROW + q4 * 4 * KW, x.v[t], 4 * KW);
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-
-    // S^T: 4 tiles of 16 tokens
-    f32x4 sc[4];
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      const uint32_t e = (uint8_t)wks[(16 * t + n) * GR + q4 * GR / 4];
-      const float ksc = __uint_as_float(e << 23);
-      sc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int s = 0; s < KW; ++s) {
-        bf16x8 kf = decode8(x.k[t][s], ksc);
-        if (__builtin_amdgcn_ballot_w64(e == kScaleNan)) {
-          const __bf16 nan = __builtin_bit_cast(__bf16, (unsigned short)0x7fc0);
-          if (e == kScaleNan) kf = bf16x8{nan, nan, nan, nan, nan, nan, nan, nan};
+      for (int c = 0; c < 2; ++c) {
+        bf16x8 x[2] = {bf16x8{}, bf16x8{}};
+        if (real) {
+          x[0] = *(const bf16x8*)(q + 64 * s + 32 * c);
+          x[1] = *(const bf16x8*)(q + 64 * s + 32 * c + 8);
         }
-        sc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[s], sc[t], 0, 0, 0);
+        e[c] = query_scale<32>(x);
+        split16(x, __uint_as_float((uint32_t)(254 - e[c]) << 23), hi + 4 * c, lo + 4 * c);
       }
-    }
-    const bool full = page_full(a, sp, kb);
-    if (!full) {
-      const int lim = row_limit(a, sp, pos, kb) - 4 * q4;
-#pragma unroll
-      for (int t = 0; t < 4; ++t)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) sc[t][r] = 16 * t + r > lim ? -INFINITY : sc[t][r];
-    }
-    float mx = sc[0][0];
-#pragma unroll
-    for (int t = 0; t < 4; ++t)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) mx = fmaxf(mx, sc[t][r]);
-    const float mnew = fmaxf(m, row_max(mx) * a.c);
-    const float alpha = mnew == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mnew);
-    const float ms = mnew == -INFINITY ? 0.f : mnew;
-    m = mnew;
-    l *= alpha;
-#pragma unroll
-    for (int c = 0; c < CT; ++c) o[c] *= alpha;
-    float p[16];
-#pragma unroll
-    for (int t = 0; t < 4; ++t)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        p[4 * t + r] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[t][r], a.c, -ms));
-        l += p[4 * t + r];
-      }
-    // V scales of this lane's tokens 16 t + 4 q4 + r
-    uint32_t ve[16];
-    bool nan_seen = false;
-#pragma unroll
-    for (int t = 0; t < 4; ++t)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const char* at = wvs + (16 * t + 4 * q4 + r) * GR;
-        ve[4 * t + r] = GR == 4 ? *(const uint32_t*)at : *(const unsigned short*)at;
-        nan_seen |= (ve[4 * t + r] & 0xff) == kScaleNan;  // all of a vector's bytes or none
-      }
-    const bool any_nan = __builtin_amdgcn_ballot_w64(nan_seen) != 0;
-#pragma unroll
-    for (int gr = 0; gr < GR; ++gr) {
-      bf16x8 pf[2];
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        float w = p[e] * __uint_as_float(((ve[e] >> (8 * gr)) & 0xff) << 23);
-        if (any_nan && ((ve[e] >> (8 * gr)) & 0xff) == kScaleNan)
-          w = sc[e / 4][e % 4] == -INFINITY ? 0.f : NAN;
-        pf[e / 8][e % 8] = (__bf16)w;
-      }
-#pragma unroll
-      for (int c2 = 0; c2 < 2; ++c2) {
-        const int ct = 2 * gr + c2;
-        const int tok = 16 * (n >> 2) + 4 * q4 + (n & 3);
-        const i32x2 w = __builtin_amdgcn_ds_read_tr4_b64_v2i32((lds_i32x2*)(wv + tok * VROW + 8 * ct));
-        o[ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(decode8((uint32_t)w[0], 1.f), pf[0], o[ct], 0, 0, 0);
-        o[ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(decode8((uint32_t)w[1], 1.f), pf[1], o[ct], 0, 0, 0);
-      }
+      se[s] = hf ? e[1] : e[0];
+      sl[s] = se[s] == kScaleNan ? kScaleNan : se[s] - 4;
+      qh[s] = i32x8{hi[0], hi[1], hi[2], hi[3], hi[4], hi[5], hi[6], hi[7]};
+      ql[s] = i32x8{lo[0], lo[1], lo[2], lo[3], lo[4], lo[5], lo[6], lo[7]};
     }
   }
-  l = row_sum(l);
 
-  // the waves' states of a row joined
-  __syncthreads();
-  float* jo = (float*)lds;                       // [wave][row][OP]
-  float* jml = jo + kWaves * kRows * OP;         // [wave][row][2]
+  // pages: the numbers of 64 list entries, one per lane, and the set of those still to come;
+  // pages that do not exist or are masked are never visited
+  int ids = -1, from = p0 - 64;
+  uint64_t todo = 0;
+  auto next_page = [&](int* kb) {  // the next page's number, or -1; kb: its place in the sequence
+    while (todo == 0) {
+      from += 64;
+      if (from >= p1) return -1;
+      const int i = from + lane;
+      ids = -1;
+      if (i < p1) {
+        const int k = span_page(sp, i);
+        ids = a.table[(size_t)b * a.M + k];
+        if (ids >= a.n_pages) ids = -1;
+        if (a.mask != nullptr && a.mask[((size_t)b * a.Hkv + g) * a.M + k] == 0) ids = -1;
+      }
+      todo = __builtin_amdgcn_ballot_w64(ids >= 0);
+    }
+    const int j = __builtin_ctzll(todo);
+    todo &= todo - 1;
+    *kb = span_page(sp, from + j);
+    return __builtin_amdgcn_readlane(ids, j);
+  };
+  auto record = [&](int id) { return a.pages + ((size_t)id * a.Hkv + g) * R::kBytes; };
+
+  // K: wave w copies a quarter (D = 64: the first two waves a half) of the codes; chunk c of
+  // token row r stands at slot c ^ (r / 4) % 4 (D = 64: c ^ (r / 8) % 2)
+  const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_addr(lds));
+  const uint32_t kc_at = lane / CPR * VROW + ((lane % CPR) ^ (D == 128 ? (lane >> 4) & 3 : (lane >> 4) & 1)) * 16;
+  auto copy_k = [&](const uint8_t* rec, int buf) {
+    if (D == 128 || wave < 2)
+      copy16_to_lds(rec + wave * 1024, kc_at, lds0 + 2 * VB + buf * KB + wave * 1024);
+  };
+  // V: thread t turns a quarter of token t / 4's codes into bf16
+  typedef unsigned Codes __attribute__((ext_vector_type(D / 32)));
+  const int vt = tid >> 2, vq = tid & 3;
+  const uint32_t vc_at = R::kV + vt * VROW + vq * (VROW / 4);
+  const uint32_t vs_at = R::kVs + vt * GR + (D == 128 ? vq : vq >> 1);
+  struct Next {
+    Codes v;
+    uint32_t vs, nan, ks[2];  // V scale of the thread's codes, of token `lane`; K scales of tokens n, 32 + n
+  } x;
+  auto load_next = [&](const uint8_t* rec) {
+    x.v = *(const Codes*)(rec + vc_at);
+    x.vs = (rec + vs_at)[0];
+    x.nan = (rec + R::kVs + GR * lane)[0];
 #pragma unroll
-  for (int c = 0; c < CT; ++c)
-    *(f32x4*)(jo + (wave * kRows + n) * OP + 16 * c + 4 * q4) = o[c];
-  if (q4 == 0) {
-    jml[(wave * kRows + n) * 2] = m;
-    jml[(wave * kRows + n) * 2 + 1] = l;
+    for (int t = 0; t < 2; ++t) {
+      if constexpr (D == 128) x.ks[t] = *(const uint32_t*)(rec + R::kKs + (32 * t + n) * GR);
+      else x.ks[t] = *(const unsigned short*)(rec + R::kKs + (32 * t + n) * GR);
+    }
+  };
+  auto store_v = [&](int buf, int kb) {
+    // bytes behind the sequence, and of tokens that stand for NaN, become 0
+    const float sc = kb * kBlk + vt < sp.keys && x.vs != kScaleNan ? __uint_as_float(x.vs << 23) : 0.f;
+    const bool zero = sc == 0.f;
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c) {
+      const bf16x8 v = decode8(zero ? 0u : x.v[c], zero ? 1.f : sc);
+      *(bf16x8*)(lds + buf * VB + tile_elem<D>(vt, vq * (D / 32) + c) * 2) = v;
+    }
+  };
+  const uint32_t kr_at = lds0 + 2 * VB + n * VROW;
+  const int ksw = D == 128 ? (n >> 2) & 3 : (n >> 3) & 1;
+  const int tg = lane >> 4, tr = (lane >> 2) & 3, tq = lane & 3;
+  const uint32_t vr_at = lds0 + (uint32_t)(tile_elem<D>(4 * (tg >> 1) + tr, 2 * (tg & 1) + (tq >> 1)) + 4 * (tq & 1)) * 2;
+  typedef const __attribute__((address_space(3))) char* lds_cp;
+  typedef const __attribute__((address_space(3))) u32x4* lds_u32x4;
+
+  f32x16 o[DT];
+#pragma unroll
+  for (int d = 0; d < DT; ++d) o[d] = f32x16{};
+  float m = -INFINITY, ms = 0.f, l = 0.f;
+
+  int kb = 0, buf = 0, kb_next = 0;
+  int id = next_page(&kb);
+  if (id >= 0) {
+    copy_k(record(id), 0);
+    load_next(record(id));
+    store_v(0, kb);
   }
+  uint32_t ks[2] = {x.ks[0], x.ks[1]};
+  uint64_t v_nan = __builtin_amdgcn_ballot_w64(x.nan == kScaleNan);
+  wait_vm<0>();
   __syncthreads();
-  constexpr int TPR = 64 * kWaves / kRows;  // threads per row
-  constexpr int EPT = D / TPR;              // elements per thread
-  const int jr = threadIdx.x / TPR, d0 = threadIdx.x % TPR * EPT;
-  if (r0 + jr >= r1) return;
+  while (id >= 0) {
+    const int id_next = next_page(&kb_next);
+    if (id_next >= 0) {
+      copy_k(record(id_next), buf ^ 1);
+      load_next(record(id_next));
+    }
+    // S^T: 2 tiles of 32 tokens
+    f32x16 sc[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      sc[t] = f32x16{};
+      const int kse = (int)(ks[t] >> (8 * hf));
+#pragma unroll
+      for (int s = 0; s < KS; ++s) {
+        const u32x4 k = *(lds_u32x4)(lds_cp)(kr_at + buf * KB + 32 * t * VROW + (((2 * s + hf) ^ ksw) * 16));
+        const i32x8 ka = {(int)k[0], (int)k[1], (int)k[2], (int)k[3], 0, 0, 0, 0};
+        if (s == 0) {
+          sc[t] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ka, qh[s], sc[t], 4, 0, 0, kse, 0, se[s]);
+          sc[t] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ka, ql[s], sc[t], 4, 0, 0, kse, 0, sl[s]);
+        } else {
+          sc[t] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ka, qh[s], sc[t], 4, 0, 2, kse, 0, se[s]);
+          sc[t] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ka, ql[s], sc[t], 4, 0, 2, kse, 0, sl[s]);
+        }
+      }
+    }
+    if (!page_full(a, sp, kb)) {
+      const int lim = row_limit(a, sp, pos, kb) - 4 * hf;
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sc[t][r] = 32 * t + 8 * (r >> 2) + (r & 3) > lim ? -INFINITY : sc[t][r];
+    }
+    // the running maximum moves only where a row's scores exceed it by 2^kTau
+    float mx = fmaxf(sc[0][0], sc[1][0]);
+#pragma unroll
+    for (int r = 1; r < 16; ++r) mx = fmaxf(fmaxf(mx, sc[0][r]), sc[1][r]);
+    if (__builtin_amdgcn_ballot_w64(mx * a.c > m + kTau)) {
+      const float mnew = fmaxf(m, other_half_max(mx) * a.c);
+      ms = mnew == -INFINITY ? 0.f : mnew;
+      const float alpha = __builtin_amdgcn_exp2f(m - ms);
+      m = mnew;
+      l *= alpha;
+#pragma unroll
+      for (int d = 0; d < DT; ++d) o[d] *= alpha;
+    }
+    uint32_t poison[2] = {0, 0};  // this lane's weights of values that stand for NaN, seen by their row
+    if (v_nan != 0) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        uint32_t set = (uint32_t)(v_nan >> (32 * t)) >> (4 * hf);
+        asm volatile("" : "+v"(set));
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          poison[t] |= (set >> (8 * (r >> 2) + (r & 3)) & 1) && sc[t][r] != -INFINITY ? 1u << r : 0u;
+      }
+    }
+    bf16x8 pa[2][2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        u32x4 u;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float w0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[t][8 * c + 2 * e], a.c, -ms));
+          const float w1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[t][8 * c + 2 * e + 1], a.c, -ms));
+          l += w0;
+          l += w1;
+          u[e] = pack_bf16(w0, w1);
+        }
+        if (v_nan != 0) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            if (poison[t] >> (8 * c + 2 * e) & 1) u[e] = (u[e] & 0xffff0000u) | 0x7fc0u;
+            if (poison[t] >> (8 * c + 2 * e + 1) & 1) u[e] = (u[e] & 0xffffu) | 0x7fc00000u;
+          }
+        }
+        pa[t][c] = __builtin_bit_cast(bf16x8, u);
+      }
+    const uint32_t vb = vr_at + buf * VB;
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int c = 0; c < 2; ++c)
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+          const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+              (lds_s16x4*)(lds_cp)((vb ^ (uint32_t)(d << 6)) + (32 * t + 16 * c) * RB));
+          const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+              (lds_s16x4*)(lds_cp)((vb ^ (uint32_t)((d << 6) | 32)) + (32 * t + 16 * c + 8) * RB));
+          const bf16x8 vf = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pa[t][c], o[d], 0, 0, 0);
+        }
+    if (id_next >= 0) {
+      store_v(buf ^ 1, kb_next);
+      ks[0] = x.ks[0];
+      ks[1] = x.ks[1];
+      v_nan = __builtin_amdgcn_ballot_w64(x.nan == kScaleNan);
+    }
+    wait_vm<0>();
+    __syncthreads();
+    id = id_next;
+    kb = kb_next;
+    buf ^= 1;
+  }
+
+  // this lane's row: channels 32 d + 8 i + 4 hf ..
+  const float ls = half_pair_sum(l);
+  if (row >= r1) return;
+  if (ca.ns > 1) {
+    const size_t at = (((size_t)unit * ca.tiles + tile) * ca.ns + seg) * kTile + 32 * wave + n;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *(f32x4*)(ca.part + at * D + 32 * d + 8 * i + 4 * hf) =
+            f32x4{o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]};
+    if (hf == 0) {
+      ca.ml[at * 2] = m;
+      ca.ml[at * 2 + 1] = ls;
+    }
+    return;
+  }
+#pragma unroll
+  for (int d = 0; d < DT; ++d)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float v[4] = {o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]};
+      store_row<4>(a, sp, D, b, g, row, 32 * d + 8 * i + 4 * hf, v, ms, ls);
+    }
+}
+
+// The segments of a tile's rows joined: a thread per row and 4 channels.
+template <int D>
+__global__ __launch_bounds__(256) void k_cache_chunk_join(CacheArgs a, ChunkArgs ca) {
+  constexpr int C = D / 4, RPW = 256 / C;  // rows of a workgroup
+  const int rows = a.S_q * a.G;
+  const long long i = (long long)blockIdx.x * RPW + threadIdx.x / C;
+  const int d0 = threadIdx.x % C * 4, unit = (int)(i / rows), r = (int)(i % rows);
+  if (unit >= a.B * a.Hkv) return;
+  const int b = unit / a.Hkv, g = unit % a.Hkv, tile = r / kTile;
+  const Span sp = make_span(a, b, 0, rows);
+  const size_t at = ((size_t)unit * ca.tiles + tile) * ca.ns * kTile + r % kTile;
   float top = -INFINITY;
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) top = fmaxf(top, jml[(w * kRows + jr) * 2]);
+  for (int s = 0; s < ca.ns; ++s) top = fmaxf(top, ca.ml[(at + (size_t)s * kTile) * 2]);
   const float ts = top == -INFINITY ? 0.f : top;
-  float den = 0.f, acc[EPT];
-#pragma unroll
-  for (int e = 0; e < EPT; ++e) acc[e] = 0.f;
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
-    const float f = __builtin_amdgcn_exp2f(jml[(w * kRows + jr) * 2] - ts);
-    den += f * jml[(w * kRows + jr) * 2 + 1];
-#pragma unroll
-    for (int e = 0; e < EPT; ++e) acc[e] += f * jo[(w * kRows + jr) * OP + d0 + e];
+  float den = 0.f;
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  for (int s = 0; s < ca.ns; ++s) {
+    const size_t p = at + (size_t)s * kTile;
+    const float f = __builtin_amdgcn_exp2f(ca.ml[p * 2] - ts);
+    den += f * ca.ml[p * 2 + 1];
+    acc += f * *(const f32x4*)(ca.part + p * D + d0);
   }
-  const int jq = (r0 + jr) / a.G, jh = g * a.G + (r0 + jr) % a.G;
-  const bool dead = jq >= sp.n || sp.first + jq < 0 || den == 0.f;
-  const float inv = dead ? 0.f : 1.f / den;
-  const size_t orow = ((size_t)b * a.Hq + jh) * a.S_q + jq;
-#pragma unroll
-  for (int e = 0; e < EPT; ++e) {
-    const float v = dead ? 0.f : acc[e] * inv;
-    if (a.out_bf16) ((__bf16*)a.out)[orow * D + d0 + e] = (__bf16)v;
-    else ((float*)a.out)[orow * D + d0 + e] = v;
+  const float v[4] = {acc[0], acc[1], acc[2], acc[3]};
+  store_row<4>(a, sp, D, b, g, r, d0, v, ts, den);
+}
+
+struct ChunkPlan {
+  int tiles, ns, grid;
+  size_t part, total;
+};
+
+ChunkPlan chunk_plan(int B, int Hkv, int rows, int D, int M) {
+  ChunkPlan p{};
+  p.tiles = (rows + kTile - 1) / kTile;
+  const long long items = (long long)B * Hkv * p.tiles;
+  long long ns = items >= 512 ? 1 : (512 + items - 1) / items;  // two workgroups per CU
+  const long long most = (M + 7) / 8;                          // 8 pages a segment at least
+  p.ns = (int)(ns < most ? ns : most);
+  p.grid = (int)(items * p.ns);
+  const size_t slots = (size_t)p.grid * kTile;
+  p.part = (slots * 2 * sizeof(float) + 255) & ~(size_t)255;
+  p.total = p.ns > 1 ? p.part + slots * D * sizeof(float) : 256;
+  return p;
+}
+
+template <int D>
+void launch_chunk(const CacheArgs& a, const ChunkPlan& p, void* ws, hipStream_t s) {
+  ChunkArgs ca{p.tiles, p.ns, (float*)((char*)ws + p.part), (float*)ws};
+  hipLaunchKernelGGL(k_cache_chunk<D>, dim3(p.grid), dim3(256), 0, s, a, ca);
+  if (p.ns > 1) {
+    const long long rows = (long long)a.B * a.Hkv * a.S_q * a.G;
+    hipLaunchKernelGGL(k_cache_chunk_join<D>, dim3((unsigned)((rows + 1024 / D - 1) / (1024 / D))), dim3(256), 0, s, a, ca);
   }
-  if (d0 == 0 && a.lse != nullptr)
-    a.lse[orow] = dead ? -INFINITY : (ts + __builtin_amdgcn_logf(den)) * 0.6931471805599453f;
 }
 
 // What a call's sizes make of it.
@@ -972,7 +1122,7 @@ void launch_token(const CacheArgs& a, const SplitArgs& sa, int groups, int rows,
 
 size_t cache_attn_ws(int B, int Hq, int Hkv, int S_q, int D, int M) {
   const int rows = S_q * (Hq / Hkv);
-  return rows <= 32 ? token_plan(B, Hkv, rows, D, M).total : 256;
+  return rows <= 32 ? token_plan(B, Hkv, rows, D, M).total : chunk_plan(B, Hkv, rows, D, M).total;
 }
 
 hipError_t launch_cache_attn(const CacheArgs& a, int D, void* ws, hipStream_t s) {
@@ -988,14 +1138,11 @@ hipError_t launch_cache_attn(const CacheArgs& a, int D, void* ws, hipStream_t s)
     }
     if (D == 64) launch_token<64>(a, sa, p.groups, rows, s);
     else launch_token<128>(a, sa, p.groups, rows, s);
-    return hipGetLastError();
+  } else {
+    const ChunkPlan p = chunk_plan(a.B, a.Hkv, rows, D, a.M);
+    if (D == 64) launch_chunk<64>(a, p, ws, s);
+    else launch_chunk<128>(a, p, ws, s);
   }
-  const int tiles = (rows + kRows - 1) / kRows;
-  const dim3 grid((unsigned)(a.B * a.Hkv * tiles));
-  if (D == 64)
-    hipLaunchKernelGGL(k_cache_attn<64>, grid, dim3(64 * kWaves), 0, s, a, tiles);
-  else
-    hipLaunchKernelGGL(k_cache_attn<128>, grid, dim3(64 * kWaves), 0, s, a, tiles);
   return hipGetLastError();
 }
 
