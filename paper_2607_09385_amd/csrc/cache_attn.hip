@@ -111,6 +111,9 @@ __device__ __forceinline__ void for_tokens(uint64_t set, int q4, F f) {
   for (int e = 0; e < 16; ++e) f(e, ((e < 8 ? lo : hi) >> (16 * (e / 4 % 2) + e % 4) & 1) != 0);
 }
 
+// A running maximum to subtract: 0 before the first key.
+__device__ __forceinline__ float finite_max(float m) { return m == -INFINITY ? 0.f : m; }
+
 // Two numbers rounded to bf16, in one register.
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
   typedef float f32x2 __attribute__((ext_vector_type(2)));
@@ -154,7 +157,7 @@ struct PageRegs {
 template <int D>
 struct QueryRegs {
   i32x8 h, l;
-  int se, sl;  // scale bytes of the 32 channels that this lane group stands for
+  int se;  // scale byte of the 32 channels that this lane group stands for; D = 128: lo's in byte 1
 };
 
 // 16 channels x, scaled by 2^-e, as 4 dwords of hi and 4 of lo.
@@ -214,8 +217,8 @@ __device__ __forceinline__ QueryRegs<D> load_query(const __bf16* q, bool real, i
     // lane group g gives the scale of channels 32 g ..: that of group 2 (g % 2)
     const int lane = threadIdx.x & 63, from = (lane & 15) | ((q4 & 1) << 5);
     const int s0 = __shfl(e0, from), s1 = __shfl(e1, from);
-    r.se = q4 < 2 ? s0 : s1;
-    r.sl = r.se == kScaleNan ? kScaleNan : r.se - 4;
+    const int e = q4 < 2 ? s0 : s1;
+    r.se = e | (e == kScaleNan ? e : e - 4) << 8;
     r.h = i32x8{hi[0], hi[1], hi[2], hi[3], hi[4], hi[5], hi[6], hi[7]};
     r.l = i32x8{lo[0], lo[1], lo[2], lo[3], lo[4], lo[5], lo[6], lo[7]};
   } else {
@@ -234,23 +237,26 @@ __device__ __forceinline__ f32x4 scores(const u32x4& k, uint32_t ks, const Query
   const i32x8 a = {(int)k[0], (int)k[1], (int)k[2], (int)k[3], 0, 0, 0, 0};
   f32x4 c = {0.f, 0.f, 0.f, 0.f};
   c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, q.h, c, 4, 0, 0, (int)ks, 0, q.se);
-  if constexpr (D == 128) c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, q.l, c, 4, 0, 0, (int)ks, 0, q.sl);
+  if constexpr (D == 128) c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, q.l, c, 4, 0, 0, (int)ks, 1, q.se);
   return c;
 }
 
-// What a list costs beyond its pages (page numbers, Q, the first page's latency, the joined
-// states), in pages: with 57 units a workgroup those of the shortest lists took 238,000 cycles
-// and the mean 123,000 where this was left out.
-constexpr int kListCost = 8;
-
 // How the live pages of a call are dealt to the workgroups: all lists one after
-// another in the order (sequence, key/value head, page), kListCost units and one for
+// another in the order (sequence, key/value head, page), `cost` units and one for
 // every page each, and workgroup w takes units [w U, (w + 1) U) of them.  A list that lies in more than one workgroup is joined
 // from partial results; a workgroup leaves at most two of them, slot 2 w for the
 // first list it touches and 2 w + 1 for the last.
+//
+// The cost stands for what a list takes beyond its pages (page numbers, Q, the first
+// page's latency, the joined states): up to 8 pages, but no more than a quarter of what a
+// workgroup gets.  Left out, the workgroups with the shortest of 64 ragged sequences'
+// lists took 238,000 cycles where the mean was 123,000.
 struct SplitArgs {
   int groups;     // workgroups of the attention kernel
-  int least;      // units per workgroup at least
+  // With a page mask: the live pages of every list, found ahead by k_cache_lists, as {place
+  // in the sequence, page number} [B * Hkv][M] and their count, or nullptr
+  const int2* list;
+  const int* counts;
   float* part;    // O [2 groups][rows][D], or nullptr: one workgroup per list, nothing is split
   float* ml;      // {m, l} [2 groups][rows]
 };
@@ -260,53 +266,83 @@ struct SplitArgs {
 struct Deal {
   int total;   // units of the call
   int unit;    // units per workgroup
-  int b;       // sequence asked for
+  int cost;    // units of a list beyond its pages
+  int set;     // set of lists asked for
   int before;  // units before it
 };
 
-__device__ __forceinline__ int list_units(const Span& s) { return s.count > 0 ? s.count + kListCost : 0; }
+__device__ __forceinline__ int list_units(int pages, int cost) { return pages > 0 ? pages + cost : 0; }
 
-// The sequence of this workgroup's first unit (seq < 0), or sequence seq.  Thread t counts
-// the sequences t per .. t per + per - 1, and the one that has the answer leaves it in LDS.
+// The deal goes over sets of lists: a sequence's (every head has the same pages), or with a
+// page mask a list each.
+__device__ __forceinline__ int deal_sets(const CacheArgs& a, const SplitArgs& sa) {
+  return sa.counts != nullptr ? a.B * a.Hkv : a.B;
+}
+// Pages of each list of set i.
+__device__ __forceinline__ int set_pages(const CacheArgs& a, const SplitArgs& sa, int i, int rows) {
+  return sa.counts != nullptr ? sa.counts[i] : make_span(a, i, 0, rows).count;
+}
+
+// The set of this workgroup's first unit (set < 0), or the one asked for.  Thread t counts the
+// sets t per .. t per + per - 1, and the one that has the answer leaves it in LDS.
 __device__ __forceinline__ Deal make_deal(const CacheArgs& a, const SplitArgs& sa, int rows,
-                                          int* lds, int seq) {
+                                          int* lds, int set) {
   constexpr int T = 64 * kWaves;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int per = (a.B + T - 1) / T, b0 = tid * per, b1 = min(b0 + per, a.B);
-  int mine = 0;
-  for (int b = b0; b < b1; ++b) mine += list_units(make_span(a, b, 0, rows)) * a.Hkv;
-  int inc = mine;
+  const int sets = deal_sets(a, sa), per = (sets + T - 1) / T, i0 = tid * per, i1 = min(i0 + per, sets);
+  const int heads = sa.counts != nullptr ? 1 : a.Hkv;
+  int pages = 0, lists = 0;
+  for (int i = i0; i < i1; ++i) {
+    const int n = set_pages(a, sa, i, rows);
+    pages += n * heads;
+    lists += n > 0 ? heads : 0;
+  }
+  int ip = pages, il = lists;
 #pragma unroll
   for (int o = 1; o < 64; o *= 2) {
-    const int y = __shfl_up(inc, o);
-    if (lane >= o) inc += y;
+    const int y = __shfl_up(ip, o), z = __shfl_up(il, o);
+    if (lane >= o) {
+      ip += y;
+      il += z;
+    }
   }
-  if (lane == 63) lds[wave] = inc;
+  if (lane == 63) {
+    lds[wave] = ip;
+    lds[kWaves + wave] = il;
+  }
   __syncthreads();
-  int before = inc - mine, total = 0;
+  int p0 = ip - pages, l0 = il - lists, tp = 0, tl = 0;
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) {
-    before += w < wave ? lds[w] : 0;
-    total += lds[w];
+    const int y = lds[w], z = lds[kWaves + w];
+    p0 += w < wave ? y : 0;
+    l0 += w < wave ? z : 0;
+    tp += y;
+    tl += z;
   }
+  tp = __builtin_amdgcn_readfirstlane(tp);
+  tl = __builtin_amdgcn_readfirstlane(tl);
   Deal d;
-  d.total = __builtin_amdgcn_readfirstlane(total);
-  d.unit = max(sa.least, (d.total + sa.groups - 1) / sa.groups);
+  d.cost = __builtin_amdgcn_readfirstlane(min(tp / sa.groups / 4, 8));
+  d.total = tp + d.cost * tl;
+  d.unit = __builtin_amdgcn_readfirstlane(max((d.total + sa.groups - 1) / sa.groups, 4));
   const long long want = (long long)blockIdx.x * d.unit;
-  if (seq < 0 ? want >= before && want < before + mine : seq >= b0 && seq < b1) {
-    for (int b = b0; b < b1; ++b) {
-      const int n = list_units(make_span(a, b, 0, rows)) * a.Hkv;
-      if (seq < 0 ? want < before + n : b == seq) {
-        lds[kWaves] = b;
-        lds[kWaves + 1] = before;
+  int before = p0 + d.cost * l0;
+  const int mine = pages + d.cost * lists;
+  if (set < 0 ? want >= before && want < before + mine : set >= i0 && set < i1) {
+    for (int i = i0; i < i1; ++i) {
+      const int n = list_units(set_pages(a, sa, i, rows), d.cost) * heads;
+      if (set < 0 ? want < before + n : i == set) {
+        lds[2 * kWaves] = i;
+        lds[2 * kWaves + 1] = before;
         break;
       }
       before += n;
     }
   }
   __syncthreads();
-  d.b = __builtin_amdgcn_readfirstlane(lds[kWaves]);
-  d.before = __builtin_amdgcn_readfirstlane(lds[kWaves + 1]);
+  d.set = __builtin_amdgcn_readfirstlane(lds[2 * kWaves]);
+  d.before = __builtin_amdgcn_readfirstlane(lds[2 * kWaves + 1]);
   __syncthreads();
   return d;
 }
@@ -364,32 +400,35 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(D, NT)) void k_cache_to
 
   int left;              // units of this workgroup
   int b, g, off;         // list and unit of it of the next one
-  bool split;
-  if (sa.part == nullptr) {
+  int cost = 0;
+  const bool split = sa.part != nullptr, listed = sa.counts != nullptr;
+  if (!split) {
     b = blockIdx.x / a.Hkv;
     g = blockIdx.x % a.Hkv;
     off = 0;
     left = 1;  // one list, whatever its length
-    split = false;
   } else {
     const Deal d = make_deal(a, sa, rows, (int*)lds, -1);
     const long long lo = (long long)blockIdx.x * d.unit;
-    left = (int)max(min((long long)d.unit, d.total - lo), 0ll);
+    left = __builtin_amdgcn_readfirstlane((int)max(min((long long)d.unit, d.total - lo), 0ll));
+    cost = d.cost;
     b = g = off = 0;
     if (left > 0) {
-      const int n = list_units(make_span(a, d.b, 0, rows)), at = (int)lo - d.before;
-      b = d.b;
-      g = __builtin_amdgcn_readfirstlane(at / n);
-      off = at - g * n;
+      const int n = list_units(set_pages(a, sa, d.set, rows), cost), at = (int)lo - d.before;
+      const int i = at / n;  // list of the set
+      b = __builtin_amdgcn_readfirstlane(listed ? d.set / a.Hkv : d.set);
+      g = __builtin_amdgcn_readfirstlane(listed ? d.set % a.Hkv : i);
+      off = __builtin_amdgcn_readfirstlane(at - i * n);
     }
-    split = true;
     // lists without a page: their rows are zero
-    for (int z = blockIdx.x; z < a.B; z += sa.groups) {
-      const Span sp = make_span(a, z, 0, rows);
-      if (sp.count > 0) continue;
+    const int sets = deal_sets(a, sa), heads = listed ? 1 : a.Hkv;
+    for (int z = blockIdx.x; z < sets; z += sa.groups) {
+      if (set_pages(a, sa, z, rows) > 0) continue;
+      const int zb = listed ? z / a.Hkv : z, zg = listed ? z % a.Hkv : 0;
+      const Span sp = make_span(a, zb, 0, rows);
       const float zero[4] = {0.f, 0.f, 0.f, 0.f};
-      for (int i = threadIdx.x; i < a.Hkv * rows * (D / 4); i += 64 * kWaves)
-        store_row<4>(a, sp, D, z, i / (D / 4) / rows, i / (D / 4) % rows, i % (D / 4) * 4, zero, 0.f, 0.f);
+      for (int i = threadIdx.x; i < heads * rows * (D / 4); i += 64 * kWaves)
+        store_row<4>(a, sp, D, zb, zg + i / (D / 4) / rows, i / (D / 4) % rows, i % (D / 4) * 4, zero, 0.f, 0.f);
     }
   }
 
@@ -400,8 +439,9 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(D, NT)) void k_cache_to
   bool first = true;
   for (; left > 0; first = false) {
     const Span sp = make_span(a, b, 0, rows);
-    const int units = list_units(sp), last = split ? min(units, off + left) : units;
-    const int begin = max(off - kListCost, 0), end = max(last - kListCost, 0);
+    const int count = __builtin_amdgcn_readfirstlane(listed ? sa.counts[b * a.Hkv + g] : sp.count);
+    const int units = list_units(count, cost), last = split ? min(units, off + left) : units;
+    const int begin = max(off - cost, 0), end = max(last - cost, 0);
 
     // this lane's query rows, and its part of Q as the B operand
     QueryRegs<D> qf[NT];
@@ -415,27 +455,30 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(D, NT)) void k_cache_to
     }
 
     f32x4 o[NT][CT];
-    float m[NT], ms[NT], l[NT];  // ms: m, or 0 before the first key
+    float m[NT], l[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
 #pragma unroll
       for (int c = 0; c < CT; ++c) o[t][c] = f32x4{0.f, 0.f, 0.f, 0.f};
       m[t] = -INFINITY;
-      ms[t] = l[t] = 0.f;
+      l[t] = 0.f;
     }
 
-    // page numbers of this wave's next 64 pages, one per lane; -1: no key of it is visible
-    int ids = -1, base = begin + wave;
+    // this wave's next 64 pages, one per lane: number (-1: no key of it is visible) and place
+    int ids = -1, places = 0, base = begin + wave;
     auto load_ids = [&](int from) {
-      const int i = from + kWaves * lane;
-      int id = -1;
-      if (i < end) {
-        const int kb = span_page(sp, i);
-        id = a.table[(size_t)b * a.M + kb];
-        if (id >= a.n_pages) id = -1;
-        if (a.mask != nullptr && a.mask[((size_t)b * a.Hkv + g) * a.M + kb] == 0) id = -1;
+      const int i = from + kWaves * (thread_here() & 63);
+      if (i >= end) return;
+      if (listed) {
+        const int2 e = sa.list[(size_t)(b * a.Hkv + g) * a.M + i];
+        places = e.x;
+        ids = e.y;
+        return;
       }
-      return id;
+      places = span_page(sp, i);
+      ids = a.table[(size_t)b * a.M + places];
+      if (ids >= a.n_pages) ids = -1;
+      if (a.mask != nullptr && a.mask[((size_t)b * a.Hkv + g) * a.M + places] == 0) ids = -1;
     };
     auto record = [&](int id) { return a.pages + ((size_t)id * a.Hkv + g) * R::kBytes; };
     // a lane's places in a record.  K, D = 64: lane groups 2 and 3 hold the channels of 0
@@ -467,15 +510,17 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(D, NT)) void k_cache_to
         copy16_to_lds(rec + j * 1024, v_at, wv_lds + buf * kVBytes + j * 1024);
     };
 
-    int id = -1, buf = 0;
+    int id = -1, buf = 0, kb_next = 0;
     if (base < end) {
-      ids = load_ids(base);
+      load_ids(base);
       id = __builtin_amdgcn_readfirstlane(ids);
+      kb_next = __builtin_amdgcn_readfirstlane(places);
       copy_v(record(max(id, 0)), 0);
       load_k(record(max(id, 0)));
     }
     for (int i = base; i < end; i += kWaves, buf ^= 1) {
       const bool there = id >= 0;  // else page 0 stands in, none of its keys visible
+      const int kb = kb_next;
       // S^T: 4 tiles of 16 tokens
       f32x4 sc[NT][4];
 #pragma unroll
@@ -496,12 +541,12 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(D, NT)) void k_cache_to
       // the next page on its way
       if (i + kWaves < end) {
         const int k = (i + kWaves - base) / kWaves;
-        if (k % 64 == 0) ids = load_ids(i + kWaves);
+        if (k % 64 == 0) load_ids(i + kWaves);
         id = __builtin_amdgcn_readlane(ids, k % 64);
+        kb_next = __builtin_amdgcn_readlane(places, k % 64);
         copy_v(record(max(id, 0)), buf ^ 1);
         load_k(record(max(id, 0)));
       }
-      const int kb = span_page(sp, i);
       const bool full = there && page_full(a, sp, kb);
       if (!full) {
 #pragma unroll
@@ -530,8 +575,7 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(D, NT)) void k_cache_to
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
           const float mnew = fmaxf(m[nt], row_max(mx[nt]) * a.c);
-          ms[nt] = mnew == -INFINITY ? 0.f : mnew;
-          const float alpha = __builtin_amdgcn_exp2f(m[nt] - ms[nt]);  // 0 before the first key
+          const float alpha = __builtin_amdgcn_exp2f(m[nt] - finite_max(mnew));  // 0 before the first key
           m[nt] = mnew;
           l[nt] *= alpha;
 #pragma unroll
@@ -551,15 +595,17 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(D, NT)) void k_cache_to
       }
       uint32_t pk[NT][8];
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
+      for (int nt = 0; nt < NT; ++nt) {
+        const float ms = finite_max(m[nt]);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[nt][e / 2][e % 2 * 2], a.c, -ms[nt]));
-          const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[nt][e / 2][e % 2 * 2 + 1], a.c, -ms[nt]));
+          const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[nt][e / 2][e % 2 * 2], a.c, -ms));
+          const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[nt][e / 2][e % 2 * 2 + 1], a.c, -ms));
           l[nt] += p0;
           l[nt] += p1;
           pk[nt][e] = pack_bf16(p0, p1);
         }
+      }
       if (v_nan != 0) {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
@@ -581,26 +627,19 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(D, NT)) void k_cache_to
         const int slot = ((ct >> 1) ^ (D == 128 ? q4 : q4 >> 1)) * 16 + (ct & 1) * 8;
         return __builtin_amdgcn_ds_read_tr4_b64_v2i32((lds_i32x2*)(wvb + tok * VROW + slot));
       };
-      // the next 32 channels' operands are read ahead of the present ones' use, and no further
-      u32x2 sv[2][4];
-      i32x2 w[2][2];
-      auto read_group = [&](int gr) {
-#pragma unroll
-        for (int t = 0; t < 4; ++t) sv[gr & 1][t] = *(const u32x2*)(wvs + 64 * gr + 16 * t + 4 * q4);
-        w[gr & 1][0] = read_v(2 * gr);
-        w[gr & 1][1] = read_v(2 * gr + 1);
-      };
-      read_group(0);
 #pragma unroll
       for (int gr = 0; gr < GR; ++gr) {
-        __builtin_amdgcn_sched_barrier(0);
-        if (gr + 1 < GR) read_group(gr + 1);
+        __builtin_amdgcn_sched_barrier(0);  // else all groups' operands are held at one time
+        u32x2 sv[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) sv[t] = *(const u32x2*)(wvs + 64 * gr + 16 * t + 4 * q4);
+        const i32x2 w[2] = {read_v(2 * gr), read_v(2 * gr + 1)};
         u32x4 u[NT][2];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            const uint32_t se = sv[gr & 1][e / 2][e % 2];
+            const uint32_t se = sv[e / 2][e % 2];
             const u16x2 y = __builtin_bit_cast(u16x2, pk[nt][e]) + __builtin_bit_cast(u16x2, se);
             u[nt][e / 4][e % 4] = __builtin_bit_cast(uint32_t, __builtin_elementwise_sub_sat(y, u16x2{0x3f80, 0x3f80}));
           }
@@ -618,7 +657,7 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(D, NT)) void k_cache_to
 #pragma unroll
         for (int c2 = 0; c2 < 2; ++c2) {
           const int ct = 2 * gr + c2;
-          const bf16x8 v0 = decode8((uint32_t)w[gr & 1][c2][0], 1.f), v1 = decode8((uint32_t)w[gr & 1][c2][1], 1.f);
+          const bf16x8 v0 = decode8((uint32_t)w[c2][0], 1.f), v1 = decode8((uint32_t)w[c2][1], 1.f);
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) {
             o[nt][ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, __builtin_bit_cast(bf16x8, u[nt][0]), o[nt][ct], 0, 0, 0);
@@ -681,12 +720,13 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(D, NT)) void k_cache_to
     if (!split) break;
     left -= last - off;
     off = 0;
-    if (++g == a.Hkv) {
-      g = 0;
-      do ++b;
-      while (b < a.B && make_span(a, b, 0, rows).count == 0);
-      if (b >= a.B) break;
-    }
+    do {  // the next list that has a page
+      if (++g == a.Hkv) {
+        g = 0;
+        ++b;
+      }
+    } while (b < a.B && (listed ? sa.counts[b * a.Hkv + g] == 0 : g == 0 && make_span(a, b, 0, rows).count == 0));
+    if (b >= a.B) break;
   }
 }
 
@@ -700,9 +740,11 @@ __global__ __launch_bounds__(64 * kWaves) void k_cache_join(CacheArgs a, SplitAr
   __shared__ float ldsl[PG], ldsm[PG];
   const int rows = a.S_q * a.G, b = blockIdx.x / a.Hkv, g = blockIdx.x % a.Hkv, r = blockIdx.y;
   const Span sp = make_span(a, b, 0, rows);
-  if (sp.count == 0) return;  // uniform over the workgroup
-  const Deal d = make_deal(a, sa, rows, (int*)lds, b);
-  const int units = list_units(sp), lo = d.before + g * units;
+  const bool listed = sa.counts != nullptr;
+  const int count = listed ? sa.counts[blockIdx.x] : sp.count;
+  if (count == 0) return;  // uniform over the workgroup
+  const Deal d = make_deal(a, sa, rows, (int*)lds, listed ? blockIdx.x : b);
+  const int units = list_units(count, d.cost), lo = d.before + (listed ? 0 : g * units);
   const int w0 = lo / d.unit, w1 = (lo + units - 1) / d.unit;
   if (w0 == w1) return;  // stored by its workgroup
   const int first = 2 * w0 + (lo == w0 * d.unit ? 0 : 1);
@@ -1090,11 +1132,34 @@ void launch_chunk(const CacheArgs& a, const ChunkPlan& p, void* ws, hipStream_t 
   }
 }
 
+// The live pages of every list, one wave each: the pages of the span that exist and whose
+// mask byte is set, in order.
+__global__ __launch_bounds__(256) void k_cache_lists(CacheArgs a, int rows, int2* list, int* counts) {
+  const int lane = threadIdx.x & 63, i = blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (i >= a.B * a.Hkv) return;
+  const int b = i / a.Hkv;
+  const Span sp = make_span(a, b, 0, rows);
+  int n = 0;
+  for (int from = 0; from < sp.count; from += 64) {
+    int kb = 0, id = -1;
+    if (from + lane < sp.count) {
+      kb = span_page(sp, from + lane);
+      id = a.mask[(size_t)i * a.M + kb] != 0 ? a.table[(size_t)b * a.M + kb] : -1;
+      if (id >= a.n_pages) id = -1;
+    }
+    const uint64_t live = __builtin_amdgcn_ballot_w64(id >= 0);
+    const int at = n + __builtin_popcountll(live & ((1ull << lane) - 1));
+    if (id >= 0) list[(size_t)i * a.M + at] = int2{kb, id};
+    n += __builtin_popcountll(live);
+  }
+  if (lane == 0) counts[i] = n;
+}
+
 // What a call's sizes make of it.
 struct TokenPlan {
   int groups;  // workgroups
   bool split;
-  size_t part, ml, total;  // workspace offsets and size in bytes
+  size_t part, list, counts, total;  // workspace offsets and size in bytes; {m, l} stand first
 };
 
 TokenPlan token_plan(int B, int Hkv, int rows, int D, int M) {
@@ -1105,19 +1170,32 @@ TokenPlan token_plan(int B, int Hkv, int rows, int D, int M) {
   p.groups = (int)(want < most_groups ? want : most_groups);
   p.split = M > 16;
   if (!p.split) p.groups = (int)lists;
-  p.ml = 0;
   const size_t slots = 2 * (size_t)p.groups * rows;
   p.part = (slots * 2 * sizeof(float) + 255) & ~(size_t)255;
-  p.total = p.split ? p.part + slots * D * sizeof(float) : 256;
+  p.list = p.part + slots * D * sizeof(float);
+  p.counts = p.list + (size_t)most * sizeof(int2);
+  p.total = p.split ? p.counts + (size_t)lists * sizeof(int) : 256;
   return p;
 }
 
 template <int D>
-void launch_token(const CacheArgs& a, const SplitArgs& sa, int groups, int rows, hipStream_t s) {
-  const dim3 grid(groups), wg(64 * kWaves);
+void launch_token(const CacheArgs& a, const TokenPlan& p, char* ws, int rows, hipStream_t s) {
+  SplitArgs sa{};
+  sa.groups = p.groups;
+  if (p.split) {
+    sa.ml = (float*)ws;
+    sa.part = (float*)(ws + p.part);
+    if (a.mask != nullptr) {
+      sa.list = (const int2*)(ws + p.list);
+      sa.counts = (const int*)(ws + p.counts);
+      hipLaunchKernelGGL(k_cache_lists, dim3((a.B * a.Hkv + 3) / 4), dim3(256), 0, s, a, rows,
+                         (int2*)(ws + p.list), (int*)(ws + p.counts));
+    }
+  }
+  const dim3 grid(p.groups), wg(64 * kWaves);
   if (rows <= 16) hipLaunchKernelGGL((k_cache_token<D, 1>), grid, wg, 0, s, a, sa);
   else hipLaunchKernelGGL((k_cache_token<D, 2>), grid, wg, 0, s, a, sa);
-  if (sa.part != nullptr) hipLaunchKernelGGL(k_cache_join<D>, dim3(a.B * a.Hkv, rows), wg, 0, s, a, sa);
+  if (p.split) hipLaunchKernelGGL(k_cache_join<D>, dim3(a.B * a.Hkv, rows), wg, 0, s, a, sa);
 }
 
 size_t cache_attn_ws(int B, int Hq, int Hkv, int S_q, int D, int M) {
@@ -1129,15 +1207,8 @@ hipError_t launch_cache_attn(const CacheArgs& a, int D, void* ws, hipStream_t s)
   const int rows = a.S_q * a.G;
   if (rows <= 32) {
     const TokenPlan p = token_plan(a.B, a.Hkv, rows, D, a.M);
-    SplitArgs sa{};
-    sa.groups = p.groups;
-    sa.least = 4;
-    if (p.split) {
-      sa.ml = (float*)((char*)ws + p.ml);
-      sa.part = (float*)((char*)ws + p.part);
-    }
-    if (D == 64) launch_token<64>(a, sa, p.groups, rows, s);
-    else launch_token<128>(a, sa, p.groups, rows, s);
+    if (D == 64) launch_token<64>(a, p, (char*)ws, rows, s);
+    else launch_token<128>(a, p, (char*)ws, rows, s);
   } else {
     const ChunkPlan p = chunk_plan(a.B, a.Hkv, rows, D, a.M);
     if (D == 64) launch_chunk<64>(a, p, ws, s);
