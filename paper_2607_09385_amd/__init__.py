@@ -83,7 +83,8 @@ def _check_bf16_rows(name, t, device):
         raise ValueError(f"{name} must be on {device} (got {t.device})")
     if t.stride(3) != 1:
         raise ValueError(f"rows of {name} must be contiguous (strides {t.stride()})")
-    return [0 if n == 1 else st for n, st in zip(t.shape[:3], t.stride()[:3])]
+    (n0, n1, n2, _), (s0, s1, s2, _) = t.shape, t.stride()
+    return 0 if n0 == 1 else s0, 0 if n1 == 1 else s1, 0 if n2 == 1 else s2
 
 
 def _check_out(out, shape, device):

@@ -16,34 +16,32 @@ into a graph.  Tensors that a call makes belong to the stream it runs on.
 """
 from __future__ import annotations
 
+import functools
 import math
 from typing import Optional
 
 from . import _lib
-from . import STEEL_OUT_BF16, _check_bf16_rows, _on, _stay, _stream_handle, _torch
-
-PAGE = 64
+from . import STEEL_OUT_BF16, _check_bf16_rows, _on, _torch
 
 
 def _ints(name, t, shape, device):
     torch = _torch()
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
-    if t.dtype != torch.int32 or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+    if t.dtype != torch.int32 or t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous int32 tensor {list(shape)} "
                          f"(got {t.dtype} {tuple(t.shape)})")
     if t.device != device:
         raise ValueError(f"{name} must be on {device} (got {t.device})")
+    return t.data_ptr()
 
 
 def _table(page_table, lens, device):
-    torch = _torch()
-    if not isinstance(page_table, torch.Tensor) or page_table.dim() != 2:
+    """(B, max_pages, pointer to the table, pointer to the lengths)."""
+    if not isinstance(page_table, _torch().Tensor) or page_table.dim() != 2:
         raise ValueError("page_table must be an int32 tensor [B, max_pages]")
     B, M = page_table.shape
-    _ints("page_table", page_table, (B, M), device)
-    _ints("lens", lens, (B,), device)
-    return B, M
+    return B, M, _ints("page_table", page_table, (B, M), device), _ints("lens", lens, (B,), device)
 
 
 def _gpu(name, t):
@@ -55,40 +53,60 @@ def _gpu(name, t):
 
 def _pool(pages):
     """(n_pages, Hkv, D) of one layer's pool."""
-    torch = _torch()
     _gpu("pages", pages)
-    if pages.dtype != torch.uint8 or pages.dim() != 3 or not pages.is_contiguous() \
+    if pages.dtype != _torch().uint8 or pages.dim() != 3 or not pages.is_contiguous() \
             or pages.shape[2] % 68 != 0:
         raise ValueError("pages must be a contiguous uint8 tensor [n_pages, Hkv, 68 * D] "
                          f"(got {pages.dtype} {tuple(pages.shape)})")
-    return pages.shape[0], pages.shape[1], pages.shape[2] // 68
+    n, h, r = pages.shape
+    return n, h, r // 68
 
 
 def _layers(pages):
     """(layers, n_pages, bytes of a page) of one pool, or of several of one size."""
-    torch = _torch()
     _gpu("pages", pages)
-    if pages.dtype != torch.uint8 or pages.dim() not in (3, 4) or not pages.is_contiguous():
+    if pages.dtype != _torch().uint8 or pages.dim() not in (3, 4) or not pages.is_contiguous():
         raise ValueError("pages must be a contiguous uint8 tensor [n_pages, Hkv, bytes] or "
                          f"[layers, n_pages, Hkv, bytes] (got {pages.dtype} {tuple(pages.shape)})")
-    return (pages.shape[0] if pages.dim() == 4 else 1, pages.shape[-3],
-            pages.shape[-2] * pages.shape[-1])
+    shape = pages.shape
+    return (shape[0] if len(shape) == 4 else 1), shape[-3], shape[-2] * shape[-1]
 
 
-def _made_on(stream, device):
-    """Scope in which tensors are allocated for the stream the call runs on."""
+def _empty(stream, like, *specs):
+    """New tensors (shape, dtype) on like's device, allocated for the stream the call runs on."""
     if stream is None:
-        return _stay
-    if stream.device != device:
+        return [like.new_empty(shape, dtype=dtype) for shape, dtype in specs]
+    if stream.device != like.device:
+        raise ValueError(f"stream must be on {like.device} (got {stream.device})")
+    with _torch().cuda.stream(stream):
+        return [like.new_empty(shape, dtype=dtype) for shape, dtype in specs]
+
+
+def _call(fn, device, stream, *args):
+    """fn(*args, stream handle) with the device current."""
+    torch = _torch()
+    if stream is None:
+        handle = torch._C._cuda_getCurrentRawStream(device.index)
+    elif stream.device != device:
         raise ValueError(f"stream must be on {device} (got {stream.device})")
-    return _torch().cuda.stream(stream)
+    else:
+        handle = int(stream.cuda_stream)
+    if torch._C._cuda_getDevice() == device.index:
+        st = fn(*args, handle)
+    else:
+        with _on(device):
+            st = fn(*args, handle)
+    if st:
+        _lib.check(st)
 
 
-def _optional(name, t, shape, device):
-    if t is None:
-        return None
-    _ints(name, t, shape, device)
-    return t.data_ptr()
+@functools.lru_cache(maxsize=256)
+def _bytes(name, *sizes):
+    """Workspace bytes that the library asks for."""
+    n = getattr(_lib.load(), name)(*sizes)
+    if n == 0:
+        raise _lib.SteelError(_lib.STEEL_ERR_INVALID_ARGUMENT, _lib.last_error())
+    return n
 
 
 def cache_pool(n_pages: int, Hkv: int, D: int, *, layers: Optional[int] = None, device=None):
@@ -107,37 +125,29 @@ def cache_append(k, v, pages, page_table, lens, *, new=None, stream=None):
     into the cache, as tokens lens[b] - new[b] + i of sequence b (``new`` int32 [B]:
     tokens of each sequence; None: S)."""
     n_pages, Hkv, D = _pool(pages)
-    B, M = _table(page_table, lens, pages.device)
-    ks = _check_bf16_rows("k", k, pages.device)
-    vs = _check_bf16_rows("v", v, pages.device)
+    device = pages.device
+    B, M, tp, lp = _table(page_table, lens, device)
+    ks = _check_bf16_rows("k", k, device)
+    vs = _check_bf16_rows("v", v, device)
     S = k.shape[2]
-    if tuple(k.shape) != (B, Hkv, S, D) or v.shape != k.shape:
+    if k.shape != (B, Hkv, S, D) or v.shape != k.shape:
         raise ValueError(f"k and v must be [{B}, {Hkv}, S, {D}] (got {tuple(k.shape)}, {tuple(v.shape)})")
-    np_ = _optional("new", new, (B,), pages.device)
-    if stream is not None:
-        _made_on(stream, pages.device)
-    with _on(pages.device):
-        st = _lib.load().steel_cache_append(
-            k.data_ptr(), v.data_ptr(), *ks, *vs, pages.data_ptr(), page_table.data_ptr(),
-            lens.data_ptr(), np_, B, Hkv, S, D, M, n_pages, _stream_handle(stream))
-    _lib.check(st)
+    _call(_lib.load().steel_cache_append, device, stream, k.data_ptr(), v.data_ptr(), *ks, *vs,
+          pages.data_ptr(), tp, lp, None if new is None else _ints("new", new, (B,), device),
+          B, Hkv, S, D, M, n_pages)
 
 
 def cache_load(pages, page_table, lens, S: int, *, start=None, stream=None):
     """Keys and values bf16 [B, Hkv, S, D] of tokens start[b] + i (``start`` int32 [B];
     None: 0), exactly as the cache holds them; rows without a token are 0."""
-    torch = _torch()
     n_pages, Hkv, D = _pool(pages)
-    B, M = _table(page_table, lens, pages.device)
-    sp = _optional("start", start, (B,), pages.device)
-    with _on(pages.device):
-        with _made_on(stream, pages.device):
-            k = torch.empty((B, Hkv, S, D), dtype=torch.bfloat16, device=pages.device)
-            v = torch.empty_like(k)
-        st = _lib.load().steel_cache_load(
-            pages.data_ptr(), page_table.data_ptr(), lens.data_ptr(), sp, k.data_ptr(),
-            v.data_ptr(), B, Hkv, S, D, M, n_pages, _stream_handle(stream))
-    _lib.check(st)
+    device = pages.device
+    B, M, tp, lp = _table(page_table, lens, device)
+    sp = None if start is None else _ints("start", start, (B,), device)
+    kv = ((B, Hkv, S, D), _torch().bfloat16)
+    k, v = _empty(stream, pages, kv, kv)
+    _call(_lib.load().steel_cache_load, device, stream, pages.data_ptr(), tp, lp, sp, k.data_ptr(),
+          v.data_ptr(), B, Hkv, S, D, M, n_pages)
     return k, v
 
 
@@ -155,48 +165,40 @@ def attn_cache(q, pages, page_table, lens, *, new=None, block_mask=None, window_
     torch = _torch()
     n_pages, Hkv, D = _pool(pages)
     device = pages.device
-    B, M = _table(page_table, lens, device)
+    B, M, tp, lp = _table(page_table, lens, device)
     qs = _check_bf16_rows("q", q, device)
-    Hq, S_q = q.shape[1], q.shape[2]
-    if q.shape[0] != B or q.shape[3] != D:
+    _, Hq, S_q, _ = q.shape
+    if q.shape != (B, Hq, S_q, D):
         raise ValueError(f"q must be [{B}, Hq, S_q, {D}] (got {tuple(q.shape)})")
-    np_ = _optional("new", new, (B,), device)
+    np_ = None if new is None else _ints("new", new, (B,), device)
     mp = None
     if block_mask is not None:
         if not isinstance(block_mask, torch.Tensor) or block_mask.dtype != torch.uint8 \
-                or tuple(block_mask.shape) != (B, Hkv, M) or not block_mask.is_contiguous() \
+                or block_mask.shape != (B, Hkv, M) or not block_mask.is_contiguous() \
                 or block_mask.device != device:
             raise ValueError(f"block_mask must be a contiguous uint8 [{B}, {Hkv}, {M}] on {device}")
         mp = block_mask.data_ptr()
-    if scale is None:
-        scale = 1.0 / math.sqrt(D)
     odt = torch.float32 if out_dtype is None else out_dtype
-    if odt not in (torch.float32, torch.bfloat16):
+    if odt is not torch.float32 and odt is not torch.bfloat16:
         raise ValueError("out_dtype must be torch.float32 or torch.bfloat16")
-    lib = _lib.load()
-    nbytes = lib.steel_attn_cache_workspace_bytes(B, Hq, Hkv, S_q, D, M)
-    if nbytes == 0:
-        raise _lib.SteelError(_lib.STEEL_ERR_INVALID_ARGUMENT, _lib.last_error())
-    with _on(device):
-        with _made_on(stream, device):
-            if out is None:
-                out = torch.empty((B, Hq, S_q, D), dtype=odt, device=device)
-            if lse is None:
-                lse = torch.empty((B, Hq, S_q), dtype=torch.float32, device=device)
-            ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
-        if out.dtype != odt or tuple(out.shape) != (B, Hq, S_q, D) or not out.is_contiguous() \
-                or out.device != device:
-            raise ValueError(f"out must be a contiguous {odt} tensor [B, Hq, S_q, D] on {device}")
-        if lse.dtype != torch.float32 or tuple(lse.shape) != (B, Hq, S_q) \
-                or not lse.is_contiguous() or lse.device != device:
-            raise ValueError(f"lse must be a contiguous float32 tensor [B, Hq, S_q] on {device}")
-        st = lib.steel_attn_cache(
-            q.data_ptr(), *qs, pages.data_ptr(), page_table.data_ptr(), lens.data_ptr(), np_, mp,
-            out.data_ptr(), lse.data_ptr(), B, Hq, Hkv, S_q, D, M, n_pages, float(scale),
-            1 if causal else 0, int(window_blocks), int(sink_blocks),
-            STEEL_OUT_BF16 if odt == torch.bfloat16 else 0, ws.data_ptr(), nbytes,
-            _stream_handle(stream))
-    _lib.check(st)
+    rows = (B, Hq, S_q)
+    if out is None:
+        out, = _empty(stream, pages, ((B, Hq, S_q, D), odt))
+    elif out.dtype != odt or out.shape != (B, Hq, S_q, D) or not out.is_contiguous() \
+            or out.device != device:
+        raise ValueError(f"out must be a contiguous {odt} tensor [B, Hq, S_q, D] on {device}")
+    if lse is None:
+        lse, = _empty(stream, pages, (rows, torch.float32))
+    elif lse.dtype != torch.float32 or lse.shape != rows or not lse.is_contiguous() \
+            or lse.device != device:
+        raise ValueError(f"lse must be a contiguous float32 tensor [B, Hq, S_q] on {device}")
+    nbytes = _bytes("steel_attn_cache_workspace_bytes", B, Hq, Hkv, S_q, D, M)
+    ws, = _empty(stream, pages, ((nbytes,), torch.uint8))
+    _call(_lib.load().steel_attn_cache, device, stream, q.data_ptr(), *qs, pages.data_ptr(), tp, lp,
+          np_, mp, out.data_ptr(), lse.data_ptr(), B, Hq, Hkv, S_q, D, M, n_pages,
+          1.0 / math.sqrt(D) if scale is None else float(scale), 1 if causal else 0,
+          int(window_blocks), int(sink_blocks), STEEL_OUT_BF16 if odt is torch.bfloat16 else 0,
+          ws.data_ptr(), nbytes)
     return out, lse
 
 
@@ -204,31 +206,17 @@ def pages_fork(page_table, lens, refs, parent, *, stream=None):
     """New rows (page_table [B_out, max_pages], lens [B_out]): row b continues old row
     parent[b] (int32 [B_out]), sharing its pages, or is empty (-1).  ``refs`` is
     updated: pages that no new row holds become free."""
-    torch = _torch()
     _gpu("page_table", page_table)
     device = page_table.device
-    B, M = _table(page_table, lens, device)
-    n_pages = refs.numel()
-    _ints("refs", refs, (n_pages,), device)
-    B_out = parent.numel()
-    _ints("parent", parent, (B_out,), device)
-    with _on(device):
-        with _made_on(stream, device):
-            table = torch.empty((B_out, M), dtype=torch.int32, device=device)
-            length = torch.empty((B_out,), dtype=torch.int32, device=device)
-        st = _lib.load().steel_pages_fork(
-            page_table.data_ptr(), lens.data_ptr(), refs.data_ptr(), parent.data_ptr(),
-            table.data_ptr(), length.data_ptr(), B, B_out, M, n_pages, _stream_handle(stream))
-    _lib.check(st)
+    B, M, tp, lp = _table(page_table, lens, device)
+    n_pages, B_out = refs.numel(), parent.numel()
+    rp = _ints("refs", refs, (n_pages,), device)
+    pp = _ints("parent", parent, (B_out,), device)
+    i32 = page_table.dtype
+    table, length = _empty(stream, page_table, ((B_out, M), i32), ((B_out,), i32))
+    _call(_lib.load().steel_pages_fork, device, stream, tp, lp, rp, pp, table.data_ptr(),
+          length.data_ptr(), B, B_out, M, n_pages)
     return table, length
-
-
-def _workspace(n_pages, B, device):
-    torch = _torch()
-    nbytes = _lib.load().steel_pages_workspace_bytes(n_pages, B)
-    if nbytes == 0:
-        raise _lib.SteelError(_lib.STEEL_ERR_INVALID_ARGUMENT, _lib.last_error())
-    return torch.empty(nbytes, dtype=torch.uint8, device=device), nbytes
 
 
 def pages_grow(page_table, lens, refs, new, *, stream=None):
@@ -237,24 +225,18 @@ def pages_grow(page_table, lens, refs, new, *, stream=None):
     pages that ``pages_copy`` has to copy before the new tokens are written (int32
     [B], -1: none; rows that write into a page which other rows hold get their own) and
     the free pages that remain (int32 [1]; negative: too few, nothing has changed)."""
-    torch = _torch()
     _gpu("page_table", page_table)
     device = page_table.device
-    B, M = _table(page_table, lens, device)
+    B, M, tp, lp = _table(page_table, lens, device)
     n_pages = refs.numel()
-    _ints("refs", refs, (n_pages,), device)
-    _ints("new", new, (B,), device)
-    with _on(device):
-        with _made_on(stream, device):
-            src = torch.empty((B,), dtype=torch.int32, device=device)
-            dst = torch.empty((B,), dtype=torch.int32, device=device)
-            left = torch.empty((1,), dtype=torch.int32, device=device)
-            ws, nbytes = _workspace(n_pages, B, device)
-        st = _lib.load().steel_pages_grow(
-            page_table.data_ptr(), lens.data_ptr(), refs.data_ptr(), new.data_ptr(),
-            src.data_ptr(), dst.data_ptr(), left.data_ptr(), B, M, n_pages, ws.data_ptr(), nbytes,
-            _stream_handle(stream))
-    _lib.check(st)
+    rp = _ints("refs", refs, (n_pages,), device)
+    np_ = _ints("new", new, (B,), device)
+    nbytes = _bytes("steel_pages_workspace_bytes", n_pages, B)
+    i32 = page_table.dtype
+    src, dst, left, ws = _empty(stream, page_table, ((B,), i32), ((B,), i32), ((1,), i32),
+                                ((nbytes // 4,), i32))
+    _call(_lib.load().steel_pages_grow, device, stream, tp, lp, rp, np_, src.data_ptr(),
+          dst.data_ptr(), left.data_ptr(), B, M, n_pages, ws.data_ptr(), nbytes)
     return src, dst, left
 
 
@@ -263,32 +245,21 @@ def pages_copy(pages, src, dst, *, stream=None):
     pool or in every layer of a [layers, ...] pool.  Destinations are distinct and no
     sources."""
     layers, n_pages, nbytes = _layers(pages)
-    n = src.numel()
-    _ints("src", src, (n,), pages.device)
-    _ints("dst", dst, (n,), pages.device)
-    with _on(pages.device):
-        if stream is not None:
-            _made_on(stream, pages.device)
-        st = _lib.load().steel_pages_copy(pages.data_ptr(), src.data_ptr(), dst.data_ptr(), n, layers,
-                                          n_pages, nbytes, _stream_handle(stream))
-    _lib.check(st)
+    n, device = src.numel(), pages.device
+    _call(_lib.load().steel_pages_copy, device, stream, pages.data_ptr(),
+          _ints("src", src, (n,), device), _ints("dst", dst, (n,), device), n, layers, n_pages, nbytes)
 
 
 def pages_compact(pages, page_table, lens, refs, *, stream=None):
     """Move the live pages (refs > 0) of a pool, or of every layer of a [layers, ...]
     pool, to its front; page_table and refs follow.  Returns their number (int32 [1])."""
-    torch = _torch()
     layers, n_pages, page_bytes = _layers(pages)
     device = pages.device
-    B, M = _table(page_table, lens, device)
-    _ints("refs", refs, (n_pages,), device)
-    with _on(device):
-        with _made_on(stream, device):
-            live = torch.empty((1,), dtype=torch.int32, device=device)
-            ws, nbytes = _workspace(n_pages, B, device)
-        st = _lib.load().steel_pages_compact(
-            pages.data_ptr(), page_table.data_ptr(), lens.data_ptr(), refs.data_ptr(),
-            live.data_ptr(), B, M, layers, n_pages, page_bytes, ws.data_ptr(), nbytes,
-            _stream_handle(stream))
-    _lib.check(st)
+    B, M, tp, lp = _table(page_table, lens, device)
+    rp = _ints("refs", refs, (n_pages,), device)
+    nbytes = _bytes("steel_pages_workspace_bytes", n_pages, B)
+    i32 = page_table.dtype
+    live, ws = _empty(stream, pages, ((1,), i32), ((nbytes // 4,), i32))
+    _call(_lib.load().steel_pages_compact, device, stream, pages.data_ptr(), tp, lp, rp,
+          live.data_ptr(), B, M, layers, n_pages, page_bytes, ws.data_ptr(), nbytes)
     return live

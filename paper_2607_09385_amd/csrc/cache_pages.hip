@@ -210,11 +210,91 @@ __global__ __launch_bounds__(1024) void k_pages_grow(int32_t* __restrict__ table
   for (int b = tid; b < B; b += T) lens[b] = max(lens[b], 0) + max(fresh[b], 0);
 }
 
+// The same for up to 1024 sequences and 2^16 pages, with one sequence per thread: what a
+// thread has loaded stays in registers, the free pages are a set of bits in LDS that is read
+// once, and each free page finds the sequence that takes it.  Latency bound (four dependent loads, two
+// scans): 64 rows and 2,600 pages 9.0 us, 19.5 with the kernel above.
+__global__ __launch_bounds__(1024) void k_pages_grow_few(int32_t* __restrict__ table,
+                                                         int32_t* __restrict__ lens,
+                                                         int32_t* __restrict__ refs,
+                                                         const int32_t* __restrict__ fresh,
+                                                         int32_t* __restrict__ src,
+                                                         int32_t* __restrict__ dst,
+                                                         int32_t* __restrict__ left, int B, int M,
+                                                         int n_pages) {
+  constexpr int T = 1024;
+  __shared__ unsigned long long free_set[T];  // bit i of word w: page 64 w + i is free
+  __shared__ int shared_id[T], off[T], have[T];
+  __shared__ int sums[T / 64];
+  __shared__ int narrow;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  if (tid == 0) narrow = 0;
+  const int len = tid < B ? max(lens[tid], 0) : 0, more = tid < B ? max(fresh[tid], 0) : 0;
+  const long long to = (long long)len + more;
+  for (int p0 = 0; p0 < n_pages; p0 += T) {
+    const int p = p0 + tid;
+    const unsigned long long f = __ballot(p < n_pages && refs[p < n_pages ? p : 0] == 0);
+    if (lane == 0) free_set[p0 / 64 + wave] = f;
+  }
+  int id = -1, holders = 0;
+  if (more > 0 && len % kBlk != 0 && pages_of(len) <= M) {
+    id = table[(size_t)tid * M + pages_of(len) - 1];
+    if (id >= 0 && id < n_pages) holders = refs[id];
+    if (holders <= 1) id = -1;
+  }
+  shared_id[tid] = id;
+  __syncthreads();
+  if (to > (long long)M * kBlk) narrow = 1;
+  bool copy = false;
+  if (id >= 0) {  // all writers copy but the last one where every holder writes
+    int writers = 0, last = -1;
+    for (int b = 0; b < B; ++b)
+      if (shared_id[b] == id) {
+        ++writers;
+        last = b;
+      }
+    copy = !(writers == holders && last == tid);
+  }
+  const int need = to > (long long)M * kBlk ? 0 : pages_of(to) - pages_of(len) + (copy ? 1 : 0);
+  int demand, total;
+  const int at = block_scan<T / 64>(need, sums, &demand);
+  off[tid] = at;
+  have[tid] = pages_of(len) | (copy ? 1 << 30 : 0);
+  unsigned long long mine = tid < (n_pages + T - 1) / T * (T / 64) ? free_set[tid] : 0;
+  int r = block_scan<T / 64>((int)__popcll(mine), sums, &total);
+  const bool fits = !narrow && total >= demand;  // the scans' barriers are behind both
+  if (tid == 0) left[0] = narrow ? INT_MIN : total - demand;
+  if (tid < B) {
+    src[tid] = fits && copy ? id : -1;
+    if (!(fits && copy)) dst[tid] = -1;
+    if (fits) lens[tid] = (int)to;
+    if (fits && copy) atomicAdd(refs + id, -1);
+  }
+  if (!fits) return;
+  for (; mine != 0 && r < demand; mine &= mine - 1, ++r) {
+    const int page = 64 * tid + __builtin_ctzll(mine);
+    int lo = 0, hi = B;  // the last b with off[b] <= r
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (off[mid] <= r) lo = mid; else hi = mid;
+    }
+    const int k = r - off[lo], held = have[lo] & ~(1 << 30);
+    const bool c = (have[lo] >> 30) & 1;
+    refs[page] = 1;
+    if (c && k == 0) dst[lo] = page;
+    table[(size_t)lo * M + held + k - (c ? 1 : 0)] = page;
+  }
+}
+
 hipError_t launch_pages_grow(int32_t* table, int32_t* lens, int32_t* refs, const int32_t* fresh,
                              int32_t* src, int32_t* dst, int32_t* left, int B, int M, int n_pages,
                              int32_t* ws, hipStream_t s) {
-  hipLaunchKernelGGL(k_pages_grow, dim3(1), dim3(1024), 0, s, table, lens, refs, fresh, src, dst,
-                     left, B, M, n_pages, ws);
+  if (B <= 1024 && n_pages <= 65536)
+    hipLaunchKernelGGL(k_pages_grow_few, dim3(1), dim3(1024), 0, s, table, lens, refs, fresh, src, dst,
+                       left, B, M, n_pages);
+  else
+    hipLaunchKernelGGL(k_pages_grow, dim3(1), dim3(1024), 0, s, table, lens, refs, fresh, src, dst,
+                       left, B, M, n_pages, ws);
   return hipGetLastError();
 }
 
@@ -326,6 +406,59 @@ __global__ __launch_bounds__(256) void k_pages_rank(const int32_t* __restrict__ 
   }
 }
 
+// Both for up to 2^16 pages: one workgroup with the live pages as a set of bits in LDS, a word of
+// 64 pages per thread (70 pages: 5.2 us against 4.8 + 6.8).
+__global__ __launch_bounds__(1024) void k_pages_rank_few(const int32_t* __restrict__ refs, int n_pages,
+                                                         int32_t* __restrict__ head,
+                                                         int32_t* __restrict__ hole,
+                                                         int32_t* __restrict__ mover,
+                                                         int32_t* __restrict__ rank,
+                                                         int32_t* __restrict__ live_out) {
+  constexpr int T = 1024;
+  __shared__ unsigned long long live_set[T];
+  __shared__ int sums[T / 64];
+  __shared__ int kept;  // live pages before page number `live`
+  const int tid = threadIdx.x;
+  for (int p0 = 0; p0 < n_pages; p0 += T) {
+    const int p = p0 + tid;
+    const unsigned long long f = __ballot(p < n_pages && refs[p < n_pages ? p : 0] > 0);
+    if ((tid & 63) == 0) live_set[p0 / 64 + (tid >> 6)] = f;
+  }
+  if (tid == 0) kept = 0;
+  __syncthreads();
+  const unsigned long long mine = tid < (n_pages + T - 1) / T * (T / 64) ? live_set[tid] : 0;
+  int live;
+  int before = block_scan<T / 64>((int)__popcll(mine), sums, &live);
+  if (live / 64 == tid) kept = before + (int)__popcll(mine & ((1ull << (live % 64)) - 1));
+  if (live == 64 * T && tid == 0) kept = live;
+  __syncthreads();
+  const int stay = kept;
+  const int p0 = 64 * tid, p1 = min(p0 + 64, n_pages);
+  if (p0 < live) {  // free pages below `live`
+    unsigned long long f = ~mine;
+    if (min(live, p1) - p0 < 64) f &= (1ull << (min(live, p1) - p0)) - 1;
+    for (int r = p0 - before; f != 0; f &= f - 1, ++r) hole[r] = p0 + __builtin_ctzll(f);
+  }
+  if (p1 > live) {  // live pages from there on
+    unsigned long long f = mine;
+    int r = before - stay;
+    if (live > p0) {
+      f &= ~((1ull << (live - p0)) - 1);
+      r = 0;
+    }
+    for (; f != 0; f &= f - 1, ++r) {
+      const int p = p0 + __builtin_ctzll(f);
+      mover[r] = p;
+      rank[p] = r;
+    }
+  }
+  if (tid == 0) {
+    head[0] = live;
+    head[1] = live - stay;
+    live_out[0] = live;
+  }
+}
+
 // The first `rows` workgroups rewrite the page table (one row each) and the first
 // of them the counts; the others copy the moved pages.
 __global__ __launch_bounds__(256) void k_pages_move(uint8_t* pages, long long layer_bytes,
@@ -373,9 +506,14 @@ hipError_t launch_pages_compact(uint8_t* pages, long long layer_bytes, long long
   const int pieces = (int)((page_bytes + kCopyPiece - 1) / kCopyPiece);
   const long long most = (long long)(n_pages / 2) * layers * pieces;  // moves <= n_pages / 2
   const int copiers = (int)(most < 2048 ? (most > 0 ? most : 1) : 2048);
-  hipLaunchKernelGGL(k_pages_count, dim3(chunks), dim3(256), 0, s, refs, n_pages, chunk_live);
-  hipLaunchKernelGGL(k_pages_rank, dim3(chunks), dim3(256), 0, s, refs, n_pages, chunk_live, head,
-                     hole, mover, rank, live);
+  if (n_pages <= 65536) {
+    hipLaunchKernelGGL(k_pages_rank_few, dim3(1), dim3(1024), 0, s, refs, n_pages, head, hole, mover,
+                       rank, live);
+  } else {
+    hipLaunchKernelGGL(k_pages_count, dim3(chunks), dim3(256), 0, s, refs, n_pages, chunk_live);
+    hipLaunchKernelGGL(k_pages_rank, dim3(chunks), dim3(256), 0, s, refs, n_pages, chunk_live, head,
+                       hole, mover, rank, live);
+  }
   hipLaunchKernelGGL(k_pages_move, dim3(B + copiers), dim3(256), 0, s, pages, layer_bytes, page_bytes,
                      layers, pieces, table, lens, refs, B, M, n_pages, head, hole, mover, rank);
   return hipGetLastError();

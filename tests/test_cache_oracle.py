@@ -191,10 +191,10 @@ def test_binding_refuses():
 def test_binding_checks_rows():
     t = torch.zeros((2, 4, 8, 64), dtype=torch.bfloat16)
     dev = t.device
-    assert steel._check_bf16_rows("q", t, dev) == [2048, 512, 64]
-    assert steel._check_bf16_rows("q", t.transpose(1, 2), dev) == [2048, 64, 512]
-    assert steel._check_bf16_rows("q", t[:1, :, :1], dev) == [0, 512, 0]
-    assert steel._check_bf16_rows("q", t[:, :1].expand(2, 4, 8, 64), dev) == [2048, 0, 64]
+    assert steel._check_bf16_rows("q", t, dev) == (2048, 512, 64)
+    assert steel._check_bf16_rows("q", t.transpose(1, 2), dev) == (2048, 64, 512)
+    assert steel._check_bf16_rows("q", t[:1, :, :1], dev) == (0, 512, 0)
+    assert steel._check_bf16_rows("q", t[:, :1].expand(2, 4, 8, 64), dev) == (2048, 0, 64)
     with pytest.raises(ValueError, match="contiguous"):
         steel._check_bf16_rows("q", t.transpose(2, 3), dev)
     with pytest.raises(ValueError, match="bfloat16"):
