@@ -955,14 +955,13 @@ __global__ __launch_bounds__(256, 2) void k_cache_chunk(CacheArgs a, ChunkArgs c
     f32x16 sc[2];
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      sc[t] = f32x16{};
       const int kse = (int)(ks[t] >> (8 * hf));
 #pragma unroll
       for (int s = 0; s < KS; ++s) {
         const u32x4 k = *(lds_u32x4)(lds_cp)(kr_at + buf * KB + 32 * t * VROW + (((2 * s + hf) ^ ksw) * 16));
         const i32x8 ka = {(int)k[0], (int)k[1], (int)k[2], (int)k[3], 0, 0, 0, 0};
         if (s == 0) {
-          sc[t] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ka, qh[s], sc[t], 4, 0, 0, kse, 0, se[s]);
+          sc[t] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ka, qh[s], f32x16{}, 4, 0, 0, kse, 0, se[s]);
           sc[t] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ka, ql[s], sc[t], 4, 0, 0, kse, 0, sl[s]);
         } else {
           sc[t] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ka, qh[s], sc[t], 4, 0, 2, kse, 0, se[s]);
@@ -1132,27 +1131,34 @@ void launch_chunk(const CacheArgs& a, const ChunkPlan& p, void* ws, hipStream_t 
   }
 }
 
-// The live pages of every list, one wave each: the pages of the span that exist and whose
-// mask byte is set, in order.
+// The live pages of every list, one workgroup each: the pages of the span that exist and
+// whose mask byte is set, in order.
 __global__ __launch_bounds__(256) void k_cache_lists(CacheArgs a, int rows, int2* list, int* counts) {
-  const int lane = threadIdx.x & 63, i = blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (i >= a.B * a.Hkv) return;
-  const int b = i / a.Hkv;
+  __shared__ int found[2][4];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = blockIdx.x, b = i / a.Hkv;
   const Span sp = make_span(a, b, 0, rows);
   int n = 0;
-  for (int from = 0; from < sp.count; from += 64) {
+  for (int from = 0, k = 0; from < sp.count; from += 256, k ^= 1) {
+    const int j = from + threadIdx.x;
     int kb = 0, id = -1;
-    if (from + lane < sp.count) {
-      kb = span_page(sp, from + lane);
-      id = a.mask[(size_t)i * a.M + kb] != 0 ? a.table[(size_t)b * a.M + kb] : -1;
-      if (id >= a.n_pages) id = -1;
+    if (j < sp.count) {
+      kb = span_page(sp, j);
+      const uint8_t live = a.mask[(size_t)i * a.M + kb];
+      id = a.table[(size_t)b * a.M + kb];
+      if (live == 0 || id >= a.n_pages) id = -1;
     }
-    const uint64_t live = __builtin_amdgcn_ballot_w64(id >= 0);
-    const int at = n + __builtin_popcountll(live & ((1ull << lane) - 1));
+    const uint64_t set = __builtin_amdgcn_ballot_w64(id >= 0);
+    if (lane == 0) found[k][wave] = __builtin_popcountll(set);
+    __syncthreads();
+    int at = n + __builtin_popcountll(set & ((1ull << lane) - 1));
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      at += w < wave ? found[k][w] : 0;
+      n += found[k][w];
+    }
     if (id >= 0) list[(size_t)i * a.M + at] = int2{kb, id};
-    n += __builtin_popcountll(live);
   }
-  if (lane == 0) counts[i] = n;
+  if (threadIdx.x == 0) counts[i] = n;
 }
 
 // What a call's sizes make of it.
@@ -1188,7 +1194,7 @@ void launch_token(const CacheArgs& a, const TokenPlan& p, char* ws, int rows, hi
     if (a.mask != nullptr) {
       sa.list = (const int2*)(ws + p.list);
       sa.counts = (const int*)(ws + p.counts);
-      hipLaunchKernelGGL(k_cache_lists, dim3((a.B * a.Hkv + 3) / 4), dim3(256), 0, s, a, rows,
+      hipLaunchKernelGGL(k_cache_lists, dim3(a.B * a.Hkv), dim3(256), 0, s, a, rows,
                          (int2*)(ws + p.list), (int*)(ws + p.counts));
     }
   }

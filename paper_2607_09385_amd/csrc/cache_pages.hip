@@ -41,6 +41,31 @@ __device__ __forceinline__ int block_scan(int x, int* lds, int* total) {
   return before + inc - x;
 }
 
+// The last i < n with x[i] <= r, x increasing from x[0] <= r.
+__device__ __forceinline__ int last_upto(const int* x, int n, int r) {
+  int lo = 0, hi = n;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (x[mid] <= r) lo = mid; else hi = mid;
+  }
+  return lo;
+}
+
+// Place of the k-th set bit.
+__device__ __forceinline__ int select_bit(unsigned long long x, int k) {
+  int at = 0;
+#pragma unroll
+  for (int w = 32; w > 0; w >>= 1) {
+    const int n = (int)__popcll(x & ((1ull << w) - 1));
+    if (k >= n) {
+      k -= n;
+      at += w;
+      x >>= w;
+    }
+  }
+  return at;
+}
+
 }  // namespace
 
 // One workgroup per row: the new row's entries and holds, the old row's releases.
@@ -190,12 +215,7 @@ __global__ __launch_bounds__(1024) void k_pages_grow(int32_t* __restrict__ table
   __threadfence();
   __syncthreads();
   for (int r = tid; r < demand; r += T) {
-    int lo = 0, hi = B;  // the last b with off[b] <= r
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (off[mid] <= r) lo = mid; else hi = mid;
-    }
-    const int b = lo, id = free_at[r], have = pages_of(lens[b]), old = src[b];
+    const int b = last_upto(off, B, r), id = free_at[r], have = pages_of(lens[b]), old = src[b];
     const int k = r - off[b];
     refs[id] = 1;
     if (old >= 0 && k == 0) {
@@ -224,7 +244,8 @@ __global__ __launch_bounds__(1024) void k_pages_grow_few(int32_t* __restrict__ t
                                                          int n_pages) {
   constexpr int T = 1024;
   __shared__ unsigned long long free_set[T];  // bit i of word w: page 64 w + i is free
-  __shared__ int shared_id[T], off[T], have[T];
+  __shared__ __attribute__((aligned(16))) int shared_id[T];
+  __shared__ int off[T], have[T], free_before[T];
   __shared__ int sums[T / 64];
   __shared__ int narrow;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -248,11 +269,16 @@ __global__ __launch_bounds__(1024) void k_pages_grow_few(int32_t* __restrict__ t
   bool copy = false;
   if (id >= 0) {  // all writers copy but the last one where every holder writes
     int writers = 0, last = -1;
-    for (int b = 0; b < B; ++b)
-      if (shared_id[b] == id) {
-        ++writers;
-        last = b;
+#pragma unroll 4
+    for (int b = 0; b < B; b += 4) {  // entries past B are -1
+      const int4 x = *(const int4*)(shared_id + b);
+      const int y[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        writers += y[u] == id ? 1 : 0;
+        last = y[u] == id ? b + u : last;
       }
+    }
     copy = !(writers == holders && last == tid);
   }
   const int need = to > (long long)M * kBlk ? 0 : pages_of(to) - pages_of(len) + (copy ? 1 : 0);
@@ -260,8 +286,9 @@ __global__ __launch_bounds__(1024) void k_pages_grow_few(int32_t* __restrict__ t
   const int at = block_scan<T / 64>(need, sums, &demand);
   off[tid] = at;
   have[tid] = pages_of(len) | (copy ? 1 << 30 : 0);
-  unsigned long long mine = tid < (n_pages + T - 1) / T * (T / 64) ? free_set[tid] : 0;
-  int r = block_scan<T / 64>((int)__popcll(mine), sums, &total);
+  const int words = (n_pages + T - 1) / T * (T / 64);
+  free_before[tid] = block_scan<T / 64>(tid < words ? (int)__popcll(free_set[tid]) : 0, sums, &total);
+  __syncthreads();
   const bool fits = !narrow && total >= demand;  // the scans' barriers are behind both
   if (tid == 0) left[0] = narrow ? INT_MIN : total - demand;
   if (tid < B) {
@@ -271,18 +298,15 @@ __global__ __launch_bounds__(1024) void k_pages_grow_few(int32_t* __restrict__ t
     if (fits && copy) atomicAdd(refs + id, -1);
   }
   if (!fits) return;
-  for (; mine != 0 && r < demand; mine &= mine - 1, ++r) {
-    const int page = 64 * tid + __builtin_ctzll(mine);
-    int lo = 0, hi = B;  // the last b with off[b] <= r
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (off[mid] <= r) lo = mid; else hi = mid;
-    }
-    const int k = r - off[lo], held = have[lo] & ~(1 << 30);
-    const bool c = (have[lo] >> 30) & 1;
+  for (int r = tid; r < demand; r += T) {
+    const int w = last_upto(free_before, words, r);
+    const int page = 64 * w + select_bit(free_set[w], r - free_before[w]);
+    const int b = last_upto(off, B, r);
+    const int k = r - off[b], held = have[b] & ~(1 << 30);
+    const bool c = (have[b] >> 30) & 1;
     refs[page] = 1;
-    if (c && k == 0) dst[lo] = page;
-    table[(size_t)lo * M + held + k - (c ? 1 : 0)] = page;
+    if (c && k == 0) dst[b] = page;
+    table[(size_t)b * M + held + k - (c ? 1 : 0)] = page;
   }
 }
 
