@@ -100,15 +100,11 @@ __device__ __forceinline__ float row_sum(float x) {
   return half_pair_sum(__uint_as_float(r[0]) + __uint_as_float(r[1]));
 }
 
-// Calls f(e) for the elements e of a lane's 16 scores (token 16 (e / 4) + 4 q4 + e % 4)
-// whose token is in the set.
-template <typename F>
-__device__ __forceinline__ void for_tokens(uint64_t set, int q4, F f) {
-  set >>= 4 * q4;
-  uint32_t lo = (uint32_t)set, hi = (uint32_t)(set >> 32);
-  asm volatile("" : "+v"(lo), "+v"(hi));  // tested where it is rarely needed, not ahead of the loop
-#pragma unroll
-  for (int e = 0; e < 16; ++e) f(e, ((e < 8 ? lo : hi) >> (16 * (e / 4 % 2) + e % 4) & 1) != 0);
+// The weights of tokens t and t + 1, NaN for those in the set that are no further than lim.
+__device__ __forceinline__ uint32_t poison_pair(uint32_t w, uint32_t set, int t, int lim) {
+  if ((set >> t & 1) && t <= lim) w = (w & 0xffff0000u) | 0x7fc0u;
+  if ((set >> (t + 1) & 1) && t + 1 <= lim) w = (w & 0xffffu) | 0x7fc00000u;
+  return w;
 }
 
 // A running maximum to subtract: 0 before the first key.
@@ -583,16 +579,6 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(D, NT)) void k_cache_to
         }
       }
       // P = 2^(S c - m) in bf16, two to a register
-      uint32_t poison[NT];  // this lane's weights of values that stand for NaN, seen by their rows
-      if (v_nan != 0) {
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) poison[nt] = 0;
-        for_tokens(v_nan, q4, [&](int e, bool in) {
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
-            poison[nt] |= in && sc[nt][e / 4][e % 4] != -INFINITY ? 1u << e : 0u;
-        });
-      }
       uint32_t pk[NT][8];
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
@@ -606,14 +592,16 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(D, NT)) void k_cache_to
           pk[nt][e] = pack_bf16(p0, p1);
         }
       }
-      if (v_nan != 0) {
+      if (v_nan != 0) {  // NaN for the weights of values that stand for NaN, where the row sees them
+        uint32_t set[2] = {(uint32_t)(v_nan >> (4 * q4)), (uint32_t)(v_nan >> (4 * q4) >> 32)};
+        asm volatile("" : "+v"(set[0]), "+v"(set[1]));  // tested where it is rarely needed
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
+        for (int nt = 0; nt < NT; ++nt) {
+          const int lim = there ? row_limit(a, sp, pos[nt], kb) - 4 * q4 : -1;
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            if (poison[nt] >> (2 * e) & 1) pk[nt][e] = (pk[nt][e] & 0xffff0000u) | 0x7fc0u;
-            if (poison[nt] >> (2 * e + 1) & 1) pk[nt][e] = (pk[nt][e] & 0xffffu) | 0x7fc00000u;
-          }
+          for (int e = 0; e < 8; ++e)  // tokens 16 (e / 2) + 2 (e % 2) of the lane's group
+            pk[nt][e] = poison_pair(pk[nt][e], set[e / 4], 16 * (e / 2 % 2) + 2 * (e % 2), lim - 32 * (e / 4));
+        }
       }
       // O^T += V^T P^T, 32 channels (one scale per token) at a time.  The scaling of P is an
       // addition to both exponents of a pair: P + (e - 127) in units of 2^7, not below 0.  A
@@ -837,7 +825,7 @@ __global__ __launch_bounds__(256, 2) void k_cache_chunk(CacheArgs a, ChunkArgs c
   const bool real = row < r1 && qi < sp.n;
   const int pos = real ? sp.first + qi : -1;
   i32x8 qh[KS], ql[KS];
-  int se[KS], sl[KS];  // scale bytes: lane half h gives those of channels 64 s + 32 h ..
+  int se[KS];  // scale bytes (lo's in byte 1): lane half h gives those of channels 64 s + 32 h ..
   {
     const __bf16* q = a.q + b * a.q_sb + (g * a.G + row % a.G) * a.q_sh + qi * a.q_ss + 16 * hf;
 #pragma unroll
@@ -853,8 +841,8 @@ __global__ __launch_bounds__(256, 2) void k_cache_chunk(CacheArgs a, ChunkArgs c
         e[c] = query_scale<32>(x);
         split16(x, __uint_as_float((uint32_t)(254 - e[c]) << 23), hi + 4 * c, lo + 4 * c);
       }
-      se[s] = hf ? e[1] : e[0];
-      sl[s] = se[s] == kScaleNan ? kScaleNan : se[s] - 4;
+      const int eh = hf ? e[1] : e[0];
+      se[s] = eh | (eh == kScaleNan ? eh : eh - 4) << 8;
       qh[s] = i32x8{hi[0], hi[1], hi[2], hi[3], hi[4], hi[5], hi[6], hi[7]};
       ql[s] = i32x8{lo[0], lo[1], lo[2], lo[3], lo[4], lo[5], lo[6], lo[7]};
     }
@@ -932,7 +920,7 @@ __global__ __launch_bounds__(256, 2) void k_cache_chunk(CacheArgs a, ChunkArgs c
   f32x16 o[DT];
 #pragma unroll
   for (int d = 0; d < DT; ++d) o[d] = f32x16{};
-  float m = -INFINITY, ms = 0.f, l = 0.f;
+  float m = -INFINITY, l = 0.f;
 
   int kb = 0, buf = 0, kb_next = 0;
   int id = next_page(&kb);
@@ -962,10 +950,10 @@ __global__ __launch_bounds__(256, 2) void k_cache_chunk(CacheArgs a, ChunkArgs c
         const i32x8 ka = {(int)k[0], (int)k[1], (int)k[2], (int)k[3], 0, 0, 0, 0};
         if (s == 0) {
           sc[t] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ka, qh[s], f32x16{}, 4, 0, 0, kse, 0, se[s]);
-          sc[t] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ka, ql[s], sc[t], 4, 0, 0, kse, 0, sl[s]);
+          sc[t] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ka, ql[s], sc[t], 4, 0, 0, kse, 1, se[s]);
         } else {
           sc[t] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ka, qh[s], sc[t], 4, 0, 2, kse, 0, se[s]);
-          sc[t] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ka, ql[s], sc[t], 4, 0, 2, kse, 0, sl[s]);
+          sc[t] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ka, ql[s], sc[t], 4, 0, 2, kse, 1, se[s]);
         }
       }
     }
@@ -982,24 +970,13 @@ __global__ __launch_bounds__(256, 2) void k_cache_chunk(CacheArgs a, ChunkArgs c
     for (int r = 1; r < 16; ++r) mx = fmaxf(fmaxf(mx, sc[0][r]), sc[1][r]);
     if (__builtin_amdgcn_ballot_w64(mx * a.c > m + kTau)) {
       const float mnew = fmaxf(m, other_half_max(mx) * a.c);
-      ms = mnew == -INFINITY ? 0.f : mnew;
-      const float alpha = __builtin_amdgcn_exp2f(m - ms);
+      const float alpha = __builtin_amdgcn_exp2f(m - finite_max(mnew));
       m = mnew;
       l *= alpha;
 #pragma unroll
       for (int d = 0; d < DT; ++d) o[d] *= alpha;
     }
-    uint32_t poison[2] = {0, 0};  // this lane's weights of values that stand for NaN, seen by their row
-    if (v_nan != 0) {
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        uint32_t set = (uint32_t)(v_nan >> (32 * t)) >> (4 * hf);
-        asm volatile("" : "+v"(set));
-#pragma unroll
-        for (int r = 0; r < 16; ++r)
-          poison[t] |= (set >> (8 * (r >> 2) + (r & 3)) & 1) && sc[t][r] != -INFINITY ? 1u << r : 0u;
-      }
-    }
+    const float ms = finite_max(m);
     bf16x8 pa[2][2];
 #pragma unroll
     for (int t = 0; t < 2; ++t)
@@ -1014,15 +991,23 @@ __global__ __launch_bounds__(256, 2) void k_cache_chunk(CacheArgs a, ChunkArgs c
           l += w1;
           u[e] = pack_bf16(w0, w1);
         }
-        if (v_nan != 0) {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            if (poison[t] >> (8 * c + 2 * e) & 1) u[e] = (u[e] & 0xffff0000u) | 0x7fc0u;
-            if (poison[t] >> (8 * c + 2 * e + 1) & 1) u[e] = (u[e] & 0xffffu) | 0x7fc00000u;
-          }
-        }
         pa[t][c] = __builtin_bit_cast(bf16x8, u);
       }
+    if (v_nan != 0) {  // NaN for the weights of values that stand for NaN, where the row sees them
+      const int lim = row_limit(a, sp, pos, kb) - 4 * hf;
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        uint32_t set = (uint32_t)(v_nan >> (32 * t)) >> (4 * hf);
+        asm volatile("" : "+v"(set));  // tested where it is rarely needed, not ahead of the loop
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          u32x4 u = __builtin_bit_cast(u32x4, pa[t][c]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) u[e] = poison_pair(u[e], set, 16 * c + 8 * (e / 2) + 2 * (e % 2), lim - 32 * t);
+          pa[t][c] = __builtin_bit_cast(bf16x8, u);
+        }
+      }
+    }
     const uint32_t vb = vr_at + buf * VB;
 #pragma unroll
     for (int t = 0; t < 2; ++t)
@@ -1072,7 +1057,7 @@ __global__ __launch_bounds__(256, 2) void k_cache_chunk(CacheArgs a, ChunkArgs c
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const float v[4] = {o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]};
-      store_row<4>(a, sp, D, b, g, row, 32 * d + 8 * i + 4 * hf, v, ms, ls);
+      store_row<4>(a, sp, D, b, g, row, 32 * d + 8 * i + 4 * hf, v, finite_max(m), ls);
     }
 }
 
