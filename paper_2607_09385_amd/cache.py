@@ -36,6 +36,12 @@ def _ints(name, t, shape, device):
     return t.data_ptr()
 
 
+def _numel(name, t):
+    if not isinstance(t, _torch().Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    return t.numel()
+
+
 def _table(page_table, lens, device):
     """(B, max_pages, pointer to the table, pointer to the lengths)."""
     if not isinstance(page_table, _torch().Tensor) or page_table.dim() != 2:
@@ -209,7 +215,7 @@ def pages_fork(page_table, lens, refs, parent, *, stream=None):
     _gpu("page_table", page_table)
     device = page_table.device
     B, M, tp, lp = _table(page_table, lens, device)
-    n_pages, B_out = refs.numel(), parent.numel()
+    n_pages, B_out = _numel("refs", refs), _numel("parent", parent)
     rp = _ints("refs", refs, (n_pages,), device)
     pp = _ints("parent", parent, (B_out,), device)
     i32 = page_table.dtype
@@ -228,7 +234,7 @@ def pages_grow(page_table, lens, refs, new, *, stream=None):
     _gpu("page_table", page_table)
     device = page_table.device
     B, M, tp, lp = _table(page_table, lens, device)
-    n_pages = refs.numel()
+    n_pages = _numel("refs", refs)
     rp = _ints("refs", refs, (n_pages,), device)
     np_ = _ints("new", new, (B,), device)
     nbytes = _bytes("steel_pages_workspace_bytes", n_pages, B)
@@ -245,7 +251,7 @@ def pages_copy(pages, src, dst, *, stream=None):
     pool or in every layer of a [layers, ...] pool.  Destinations are distinct and no
     sources."""
     layers, n_pages, nbytes = _layers(pages)
-    n, device = src.numel(), pages.device
+    n, device = _numel("src", src), pages.device
     _call(_lib.load().steel_pages_copy, device, stream, pages.data_ptr(),
           _ints("src", src, (n,), device), _ints("dst", dst, (n,), device), n, layers, n_pages, nbytes)
 

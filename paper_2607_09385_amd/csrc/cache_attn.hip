@@ -526,10 +526,12 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(D, NT)) void k_cache_to
         sc[nt][2] = scores<D>(x.k2, x.ks2, qf[nt]);
         sc[nt][3] = scores<D>(x.k3, x.ks3, qf[nt]);
       }
-      // all scale bytes of a vector are 255, or none: tokens that stand for NaN
-      const uint64_t v_nan = __builtin_amdgcn_ballot_w64((x.vs & 0xff) == kScaleNan);
-      const bool v_large = __builtin_amdgcn_ballot_w64((x.vs & (x.vs << 1) & 0x80808080u) != 0) != 0;
-      const uint32_t vs = (x.vs & 0xff) == kScaleNan ? 0x7f7f7f7fu : x.vs;
+      // tokens whose values stand for NaN (all scale bytes 255, or none), and whether any value is
+      // above 2^64; bytes behind the sequence count as 0
+      uint32_t vs = kb * kBlk + lane < sp.keys ? x.vs : 0u;
+      const uint64_t v_nan = __builtin_amdgcn_ballot_w64((vs & 0xff) == kScaleNan);
+      const bool v_large = __builtin_amdgcn_ballot_w64((vs & (vs << 1) & 0x80808080u) != 0) != 0;
+      vs = (vs & 0xff) == kScaleNan ? 0x7f7f7f7fu : vs;
 #pragma unroll
       for (int gr = 0; gr < GR; ++gr)
         wvs[64 * gr + lane] = (unsigned short)((vs >> (8 * gr) & 0xff) << 7);
@@ -555,7 +557,9 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(D, NT)) void k_cache_to
         }
       }
       // The running maximum moves only where a row's scores exceed it by 2^kTau: m
-      // cancels in O / l, and weights up to 2^8 lose nothing in bf16.
+      // cancels in O / l, and weights up to 2^8 lose nothing in bf16.  With values above 2^64
+      // it moves at once, so that no weight times a value leaves the range of fp32.
+      const float tau = v_large ? 0.f : kTau;
       bool grow = false;
       float mx[NT];
 #pragma unroll
@@ -565,7 +569,7 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(D, NT)) void k_cache_to
         for (int t = 0; t < 4; ++t)
 #pragma unroll
           for (int r = 0; r < 4; ++r) mx[nt] = fmaxf(mx[nt], sc[nt][t][r]);
-        grow |= mx[nt] * a.c > m[nt] + kTau;
+        grow |= mx[nt] * a.c > m[nt] + tau;
       }
       if (__builtin_amdgcn_ballot_w64(grow)) {
 #pragma unroll
@@ -888,12 +892,13 @@ __global__ __launch_bounds__(256, 2) void k_cache_chunk(CacheArgs a, ChunkArgs c
   const uint32_t vs_at = R::kVs + vt * GR + (D == 128 ? vq : vq >> 1);
   struct Next {
     Codes v;
-    uint32_t vs, nan, ks[2];  // V scale of the thread's codes, of token `lane`; K scales of tokens n, 32 + n
+    uint32_t vs, vt, ks[2];  // V scale of the thread's codes, scales of token `lane`; K scales of tokens n, 32 + n
   } x;
   auto load_next = [&](const uint8_t* rec) {
     x.v = *(const Codes*)(rec + vc_at);
     x.vs = (rec + vs_at)[0];
-    x.nan = (rec + R::kVs + GR * lane)[0];
+    if constexpr (D == 128) x.vt = *(const uint32_t*)(rec + R::kVs + GR * lane);
+    else x.vt = *(const unsigned short*)(rec + R::kVs + GR * lane);
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       if constexpr (D == 128) x.ks[t] = *(const uint32_t*)(rec + R::kKs + (32 * t + n) * GR);
@@ -930,7 +935,16 @@ __global__ __launch_bounds__(256, 2) void k_cache_chunk(CacheArgs a, ChunkArgs c
     store_v(0, kb);
   }
   uint32_t ks[2] = {x.ks[0], x.ks[1]};
-  uint64_t v_nan = __builtin_amdgcn_ballot_w64(x.nan == kScaleNan);
+  // tokens whose values stand for NaN (all scale bytes 255, or none), and whether any value is
+  // above 2^64; bytes behind the sequence count as 0
+  uint64_t v_nan = 0;
+  bool v_large = false;
+  auto look_at_v = [&](int kb) {
+    const uint32_t vt = kb * kBlk + lane < sp.keys ? x.vt : 0u;
+    v_nan = __builtin_amdgcn_ballot_w64((vt & 0xff) == kScaleNan);
+    v_large = __builtin_amdgcn_ballot_w64((vt & (vt << 1) & 0x80808080u) != 0) != 0;
+  };
+  look_at_v(kb);
   wait_vm<0>();
   __syncthreads();
   while (id >= 0) {
@@ -964,11 +978,11 @@ __global__ __launch_bounds__(256, 2) void k_cache_chunk(CacheArgs a, ChunkArgs c
 #pragma unroll
         for (int r = 0; r < 16; ++r) sc[t][r] = 32 * t + 8 * (r >> 2) + (r & 3) > lim ? -INFINITY : sc[t][r];
     }
-    // the running maximum moves only where a row's scores exceed it by 2^kTau
+    // the running maximum, as in k_cache_token
     float mx = fmaxf(sc[0][0], sc[1][0]);
 #pragma unroll
     for (int r = 1; r < 16; ++r) mx = fmaxf(fmaxf(mx, sc[0][r]), sc[1][r]);
-    if (__builtin_amdgcn_ballot_w64(mx * a.c > m + kTau)) {
+    if (__builtin_amdgcn_ballot_w64(mx * a.c > m + (v_large ? 0.f : kTau))) {
       const float mnew = fmaxf(m, other_half_max(mx) * a.c);
       const float alpha = __builtin_amdgcn_exp2f(m - finite_max(mnew));
       m = mnew;
@@ -1026,7 +1040,7 @@ __global__ __launch_bounds__(256, 2) void k_cache_chunk(CacheArgs a, ChunkArgs c
       store_v(buf ^ 1, kb_next);
       ks[0] = x.ks[0];
       ks[1] = x.ks[1];
-      v_nan = __builtin_amdgcn_ballot_w64(x.nan == kScaleNan);
+      look_at_v(kb_next);
     }
     wait_vm<0>();
     __syncthreads();

@@ -364,7 +364,8 @@ int check_pages(int B, int max_pages, int n_pages) {
   if (B < 1 || max_pages < 1 || n_pages < 1)
     return fail(STEEL_ERR_INVALID_ARGUMENT, "sizes must be >= 1 (B=%d max_pages=%d n_pages=%d)", B,
                 max_pages, n_pages);
-  if (max_pages > (1 << 24) || n_pages > steel::kMaxPages || (long long)B * max_pages > INT32_MAX)
+  if (B > (1 << 24) || max_pages > (1 << 24) || n_pages > steel::kMaxPages ||
+      (long long)B * max_pages > INT32_MAX)
     return fail(STEEL_ERR_UNSUPPORTED,
                 "B=%d rows of max_pages=%d, n_pages=%d: too large (2^31 entries, 2^24 a row, %d pages)",
                 B, max_pages, n_pages, steel::kMaxPages);

@@ -285,6 +285,89 @@ def test_bytes_behind_the_length_and_nan(S, D):
         assert np.array_equal(got[:, :2], base[0].cpu().double().numpy()[:, :2])
 
 
+@pytest.mark.parametrize("D,Hq,H,S", [(64, 16, 1, 1), (128, 17, 1, 1), (64, 32, 1, 1), (128, 33, 1, 1),
+                                      (128, 16, 1, 4), (64, 48, 1, 1), (128, 127, 1, 1), (64, 43, 1, 3)])
+def test_rows_around_the_tiles(D, Hq, H, S):
+    """16, 17, 32, 33, 64, 127 and 129 rows of one key/value head."""
+    rng = np.random.default_rng(Hq)
+    lens = np.array([1500, 200])
+    pool, table = random_pool(rng, 30, H, D), random_table(rng, lens, 30)
+    check_attention("tiles", pool, table, lens, bf16(rng, (2, Hq, S, D)), D ** -0.5)
+
+
+@pytest.mark.parametrize("D,S", [(64, 1), (128, 2), (64, 50), (128, 50)])
+def test_queries_that_are_not_finite(D, S):
+    """They make their own rows NaN; in padding they are not read."""
+    rng = np.random.default_rng(D)
+    lens, H = np.array([300, 70]), 2
+    pool, table = random_pool(rng, 9, H, D), random_table(rng, lens, 9)
+    q = bf16(rng, (2, 8, S, D))
+    s = steel()
+    args = (gpu(pool), ints(table), ints(lens))
+    clean, cl = s.attn_cache(gpu(q), *args)
+    bad = q.clone()
+    bad[0, 3, 0, 7] = float("nan")
+    bad[1, 6, S - 1, D - 1] = float("inf")
+    bad[1, 1, 0, 33] = -float("inf")
+    out, lse = s.attn_cache(gpu(bad), *args)
+    rows = torch.zeros((2, 8, S), dtype=torch.bool, device=DEV)
+    rows[0, 3, 0] = rows[1, 6, S - 1] = rows[1, 1, 0] = True
+    assert torch.isnan(out[rows]).all() and torch.isnan(lse[rows]).all()
+    assert torch.equal(out[~rows], clean[~rows]) and torch.equal(lse[~rows], cl[~rows])
+    if S > 1:
+        new = ints([1, S - 1])
+        pad = q.clone()
+        pad[0, :, 1:] = float("nan")
+        pad[1, :, S - 1:] = float("inf")
+        a = s.attn_cache(gpu(pad), *args, new=new)
+        b = s.attn_cache(gpu(q), *args, new=new)
+        assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1]) and not torch.isnan(a[0]).any()
+
+
+@pytest.mark.parametrize("D,S", [(64, 1), (128, 1), (128, 40), (64, 40)])
+def test_values_of_every_size(D, S):
+    """Scales from 2^-90 to 2^120 next to each other, keys included where scores allow it, and
+    future tokens of the largest scales."""
+    rng = np.random.default_rng(D + S)
+    lens = np.array([700, 130, S])
+    P = 20
+    pool, table = random_pool(rng, P, 2, D), random_table(rng, lens, P)
+    pool[..., 66 * D:] = rng.integers(37, 248, (P, 2, 2 * D))
+    q = bf16(rng, (3, 8, S, D))
+    check_attention("large", pool, table, lens, q, D ** -0.5)
+    # one size per sequence: the small ones keep their precision
+    for b, e in enumerate((40, 127, 250)):
+        pool[table[b][table[b] >= 0], :, 66 * D:] = e
+    check_attention("one size each", pool, table, lens, q, D ** -0.5)
+    pool[..., 66 * D:] = rng.integers(122, 129, (P, 2, 2 * D))
+    base = check_attention("plain", pool, table, lens, q, D ** -0.5)
+    plain = pool.copy()
+    if S > 1:  # the last token's value is large: only the last query sees it
+        page, tok = table[0, 10], 699 % 64
+        pool[page, :, 66 * D:].reshape(2, 64, D // 32)[:, tok] = 252
+        pool[page, :, 32 * D:64 * D].reshape(2, 64, D // 2)[:, tok] = 0x77
+        s = steel()
+        out, _ = s.attn_cache(gpu(q), gpu(pool), ints(table), ints(lens), scale=D ** -0.5)
+        # The page's large value moves the maximum of its rows at once, and rows of one wave
+        # move it together, so the others' weights may round elsewhere: both results are
+        # within u = 2^-8 of sum p |v| (u / 10 covers the fp32 terms), 2 u of each other.
+        mag = plain.copy()
+        mag[..., 32 * D:64 * D] &= 0x77
+        spread, _ = kv.attention(q.double().numpy(), mag, table, lens, D ** -0.5)
+        off = np.abs(out.cpu().double().numpy() - base[0].cpu().double().numpy())
+        assert (off[0, :, :S - 1] <= 2 * 1.1 * 2.0 ** -8 * spread[0, :, :S - 1]).all()
+
+
+@pytest.mark.parametrize("S", [1, 60])
+def test_lengths_beyond_the_table(S):
+    """Keys end with the table, positions do not."""
+    rng = np.random.default_rng(S)
+    pool, table = random_pool(rng, 12, 2, 64), rng.permutation(12).reshape(3, 4).astype(np.int32)
+    lens = np.array([256, 300, 2 ** 31 - 1])
+    for kw in ({}, {"causal": False}, {"window_blocks": 2, "sink_blocks": 1}):
+        check_attention("beyond", pool, table, lens, bf16(rng, (3, 4, S, 64)), 0.125, **kw)
+
+
 @pytest.mark.parametrize("D,S", [(64, 1), (128, 1), (128, 40)])
 def test_sharp_and_flat_scores(D, S):
     """Scores of hundreds (one key takes all), far below zero, and all equal."""
@@ -425,7 +508,8 @@ def test_fork(B_in, B_out, M, P):
 
 
 @pytest.mark.parametrize("B,M,P,most", [(1, 4, 6, 1), (5, 9, 60, 3), (40, 20, 900, 65), (200, 5, 500, 1),
-                                        (1500, 4, 6000, 70), (3, 40, 9000, 800), (16, 30, 100, 200)])
+                                        (1500, 4, 6000, 70), (3, 40, 9000, 800), (16, 30, 100, 200), (20, 30, 65536, 200),
+                                        (20, 30, 70001, 200), (1024, 3, 4000, 2), (1025, 3, 4000, 2)])
 @pytest.mark.parametrize("seed", [0, 1])
 def test_grow(B, M, P, most, seed):
     rng = np.random.default_rng(B + 1000 * seed)
@@ -474,7 +558,8 @@ def test_copy(layers, P, H, D, n):
 
 
 @pytest.mark.parametrize("layers,B,M,P", [(1, 1, 2, 3), (2, 5, 9, 70), (1, 30, 30, 1000), (1, 40, 200, 9000),
-                                          (1, 3, 2, 4096), (1, 300, 20, 12289)])
+                                          (1, 3, 2, 4096), (1, 300, 20, 12289), (1, 200, 300, 65536),
+                                          (1, 200, 300, 70003)])
 @pytest.mark.parametrize("crowded", [False, True])
 def test_compact(layers, B, M, P, crowded):
     rng = np.random.default_rng(P + crowded)
