@@ -433,8 +433,8 @@ int steel_cache_load(const uint8_t* pages, const int32_t* page_table, const int3
  * sum of weights times values, n times the mean at most, has to be an fp32 number.
  * Results are bitwise reproducible run to run.
  *
- *   workspace   at least steel_attn_cache_workspace_bytes of the same sizes
- *               (0 after an argument error)
+ *   workspace   at least steel_attn_cache_workspace_bytes of the same sizes (0 after an
+ *               argument error); where that is 256 none is used and it may be NULL
  */
 size_t steel_attn_cache_workspace_bytes(int B, int Hq, int Hkv, int S_q, int D, int max_pages);
 

@@ -199,12 +199,14 @@ def attn_cache(q, pages, page_table, lens, *, new=None, block_mask=None, window_
             or lse.device != device:
         raise ValueError(f"lse must be a contiguous float32 tensor [B, Hq, S_q] on {device}")
     nbytes = _bytes("steel_attn_cache_workspace_bytes", B, Hq, Hkv, S_q, D, M)
-    ws, = _empty(stream, pages, ((nbytes,), torch.uint8))
+    ws = None  # 256 bytes: none is used
+    if nbytes > 256:
+        ws, = _empty(stream, pages, ((nbytes,), torch.uint8))
     _call(_lib.load().steel_attn_cache, device, stream, q.data_ptr(), *qs, pages.data_ptr(), tp, lp,
           np_, mp, out.data_ptr(), lse.data_ptr(), B, Hq, Hkv, S_q, D, M, n_pages,
           1.0 / math.sqrt(D) if scale is None else float(scale), 1 if causal else 0,
           int(window_blocks), int(sink_blocks), STEEL_OUT_BF16 if odt is torch.bfloat16 else 0,
-          ws.data_ptr(), nbytes)
+          None if ws is None else ws.data_ptr(), nbytes)
     return out, lse
 
 
@@ -239,8 +241,8 @@ def pages_grow(page_table, lens, refs, new, *, stream=None):
     np_ = _ints("new", new, (B,), device)
     nbytes = _bytes("steel_pages_workspace_bytes", n_pages, B)
     i32 = page_table.dtype
-    src, dst, left, ws = _empty(stream, page_table, ((B,), i32), ((B,), i32), ((1,), i32),
-                                ((nbytes // 4,), i32))
+    n = nbytes // 4
+    ws, src, dst, left = _empty(stream, page_table, ((n + 2 * B + 1,), i32))[0].split((n, B, B, 1))
     _call(_lib.load().steel_pages_grow, device, stream, tp, lp, rp, np_, src.data_ptr(),
           dst.data_ptr(), left.data_ptr(), B, M, n_pages, ws.data_ptr(), nbytes)
     return src, dst, left
@@ -265,7 +267,7 @@ def pages_compact(pages, page_table, lens, refs, *, stream=None):
     rp = _ints("refs", refs, (n_pages,), device)
     nbytes = _bytes("steel_pages_workspace_bytes", n_pages, B)
     i32 = page_table.dtype
-    live, ws = _empty(stream, pages, ((1,), i32), ((nbytes // 4,), i32))
+    ws, live = _empty(stream, pages, ((nbytes // 4 + 1,), i32))[0].split((nbytes // 4, 1))
     _call(_lib.load().steel_pages_compact, device, stream, pages.data_ptr(), tp, lp, rp,
           live.data_ptr(), B, M, layers, n_pages, page_bytes, ws.data_ptr(), nbytes)
     return live

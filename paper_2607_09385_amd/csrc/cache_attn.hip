@@ -238,13 +238,15 @@ __device__ __forceinline__ f32x4 scores(const u32x4& k, uint32_t ks, const Query
 }
 
 // How the live pages of a call are dealt to the workgroups: all lists one after
-// another in the order (sequence, key/value head, page), `cost` units and one for
-// every page each, and workgroup w takes units [w U, (w + 1) U) of them.  A list that lies in more than one workgroup is joined
+// another in the order (sequence, key/value head, page), and workgroup w takes units
+// [w U, (w + 1) U) of them.  A list that lies in more than one workgroup is joined
 // from partial results; a workgroup leaves at most two of them, slot 2 w for the
 // first list it touches and 2 w + 1 for the last.
 //
-// The cost stands for what a list takes beyond its pages (page numbers, Q, the first
-// page's latency, the joined states): up to 8 pages, but no more than a quarter of what a
+// Few lists (a quarter of the workgroups at most): U is a multiple of the waves and every
+// list is filled up to a multiple of U, so a workgroup has one list only.  Many: a list counts
+// `cost` units beyond its pages for what it takes besides (page numbers, Q, the first
+// page's latency, the joined states): up to 8, but no more than a quarter of what a
 // workgroup gets.  Left out, the workgroups with the shortest of 64 ragged sequences'
 // lists took 238,000 cycles where the mean was 123,000.
 struct SplitArgs {
@@ -255,6 +257,7 @@ struct SplitArgs {
   const int* counts;
   float* part;    // O [2 groups][rows][D], or nullptr: one workgroup per list, nothing is split
   float* ml;      // {m, l} [2 groups][rows]
+  int2* where;    // [B * Hkv] first and last slot of a list's partial results (equal: none)
 };
 
 // Where the units of a call lie, fewer than 2^31: computed by every workgroup from the
@@ -262,12 +265,16 @@ struct SplitArgs {
 struct Deal {
   int total;   // units of the call
   int unit;    // units per workgroup
-  int cost;    // units of a list beyond its pages
+  int cost;    // units of a list beyond its pages, or
+  int fill;    //   the unit that lists are filled up to (else 1)
   int set;     // set of lists asked for
   int before;  // units before it
 };
 
-__device__ __forceinline__ int list_units(int pages, int cost) { return pages > 0 ? pages + cost : 0; }
+// Units of a list; a list's pages follow its `cost` first ones.
+__device__ __forceinline__ int list_units(int pages, int cost, int fill) {
+  return pages > 0 ? (pages + cost + fill - 1) / fill * fill : 0;
+}
 
 // The deal goes over sets of lists: a sequence's (every head has the same pages), or with a
 // page mask a list each.
@@ -279,66 +286,80 @@ __device__ __forceinline__ int set_pages(const CacheArgs& a, const SplitArgs& sa
   return sa.counts != nullptr ? sa.counts[i] : make_span(a, i, 0, rows).count;
 }
 
-// The set of this workgroup's first unit (set < 0), or the one asked for.  Thread t counts the
-// sets t per .. t per + per - 1, and the one that has the answer leaves it in LDS.
-__device__ __forceinline__ Deal make_deal(const CacheArgs& a, const SplitArgs& sa, int rows,
-                                          int* lds, int set) {
+// The set of this workgroup's first unit.  Thread t counts the sets t per .. t per + per - 1, and
+// the one that has the answer leaves it in LDS.
+__device__ __forceinline__ Deal make_deal(const CacheArgs& a, const SplitArgs& sa, int rows, int* lds) {
   constexpr int T = 64 * kWaves;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int sets = deal_sets(a, sa), per = (sets + T - 1) / T, i0 = tid * per, i1 = min(i0 + per, sets);
   const int heads = sa.counts != nullptr ? 1 : a.Hkv;
+  // pages and lists of the call
   int pages = 0, lists = 0;
   for (int i = i0; i < i1; ++i) {
     const int n = set_pages(a, sa, i, rows);
     pages += n * heads;
     lists += n > 0 ? heads : 0;
   }
-  int ip = pages, il = lists;
 #pragma unroll
-  for (int o = 1; o < 64; o *= 2) {
-    const int y = __shfl_up(ip, o), z = __shfl_up(il, o);
-    if (lane >= o) {
-      ip += y;
-      il += z;
-    }
+  for (int o = 32; o > 0; o >>= 1) {
+    pages += __shfl_xor(pages, o);
+    lists += __shfl_xor(lists, o);
   }
-  if (lane == 63) {
-    lds[wave] = ip;
-    lds[kWaves + wave] = il;
+  if (lane == 0) {
+    lds[wave] = pages;
+    lds[kWaves + wave] = lists;
   }
   __syncthreads();
-  int p0 = ip - pages, l0 = il - lists, tp = 0, tl = 0;
+  int tp = 0, tl = 0;
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) {
-    const int y = lds[w], z = lds[kWaves + w];
-    p0 += w < wave ? y : 0;
-    l0 += w < wave ? z : 0;
-    tp += y;
-    tl += z;
+    tp += lds[w];
+    tl += lds[kWaves + w];
   }
-  tp = __builtin_amdgcn_readfirstlane(tp);
-  tl = __builtin_amdgcn_readfirstlane(tl);
   Deal d;
-  d.cost = __builtin_amdgcn_readfirstlane(min(tp / sa.groups / 4, 8));
-  d.total = tp + d.cost * tl;
-  d.unit = __builtin_amdgcn_readfirstlane(max((d.total + sa.groups - 1) / sa.groups, 4));
+  if (4 * tl <= sa.groups) {
+    const int u = (tp + sa.groups - tl - 1) / (sa.groups - tl);  // the lists' last units fill at most tl more
+    d.cost = 0;
+    d.unit = d.fill = __builtin_amdgcn_readfirstlane(max((u + kWaves - 1) / kWaves * kWaves, kWaves));
+  } else {
+    d.cost = __builtin_amdgcn_readfirstlane(min(tp / sa.groups / 4, 8));
+    d.fill = 1;
+    d.unit = __builtin_amdgcn_readfirstlane(max((tp + d.cost * tl + sa.groups - 1) / sa.groups, kWaves));
+  }
+  // units before this thread's sets
+  int units = 0;
+  for (int i = i0; i < i1; ++i) units += list_units(set_pages(a, sa, i, rows), d.cost, d.fill) * heads;
+  int inc = units;
+#pragma unroll
+  for (int o = 1; o < 64; o *= 2) {
+    const int y = __shfl_up(inc, o);
+    if (lane >= o) inc += y;
+  }
+  if (lane == 63) lds[2 * kWaves + wave] = inc;
+  __syncthreads();
+  int before = inc - units, total = 0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    const int y = lds[2 * kWaves + w];
+    before += w < wave ? y : 0;
+    total += y;
+  }
+  d.total = __builtin_amdgcn_readfirstlane(total);
   const long long want = (long long)blockIdx.x * d.unit;
-  int before = p0 + d.cost * l0;
-  const int mine = pages + d.cost * lists;
-  if (set < 0 ? want >= before && want < before + mine : set >= i0 && set < i1) {
+  if (want >= before && want < before + units) {
     for (int i = i0; i < i1; ++i) {
-      const int n = list_units(set_pages(a, sa, i, rows), d.cost) * heads;
-      if (set < 0 ? want < before + n : i == set) {
-        lds[2 * kWaves] = i;
-        lds[2 * kWaves + 1] = before;
+      const int n = list_units(set_pages(a, sa, i, rows), d.cost, d.fill) * heads;
+      if (want < before + n) {
+        lds[3 * kWaves] = i;
+        lds[3 * kWaves + 1] = before;
         break;
       }
       before += n;
     }
   }
   __syncthreads();
-  d.set = __builtin_amdgcn_readfirstlane(lds[2 * kWaves]);
-  d.before = __builtin_amdgcn_readfirstlane(lds[2 * kWaves + 1]);
+  d.set = __builtin_amdgcn_readfirstlane(lds[3 * kWaves]);
+  d.before = __builtin_amdgcn_readfirstlane(lds[3 * kWaves + 1]);
   __syncthreads();
   return d;
 }
@@ -396,7 +417,7 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(D, NT)) void k_cache_to
 
   int left;              // units of this workgroup
   int b, g, off;         // list and unit of it of the next one
-  int cost = 0;
+  int cost = 0, fill = 1;
   const bool split = sa.part != nullptr, listed = sa.counts != nullptr;
   if (!split) {
     b = blockIdx.x / a.Hkv;
@@ -404,13 +425,14 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(D, NT)) void k_cache_to
     off = 0;
     left = 1;  // one list, whatever its length
   } else {
-    const Deal d = make_deal(a, sa, rows, (int*)lds, -1);
+    const Deal d = make_deal(a, sa, rows, (int*)lds);
     const long long lo = (long long)blockIdx.x * d.unit;
     left = __builtin_amdgcn_readfirstlane((int)max(min((long long)d.unit, d.total - lo), 0ll));
     cost = d.cost;
+    fill = d.fill;
     b = g = off = 0;
     if (left > 0) {
-      const int n = list_units(set_pages(a, sa, d.set, rows), cost), at = (int)lo - d.before;
+      const int n = list_units(set_pages(a, sa, d.set, rows), cost, fill), at = (int)lo - d.before;
       const int i = at / n;  // list of the set
       b = __builtin_amdgcn_readfirstlane(listed ? d.set / a.Hkv : d.set);
       g = __builtin_amdgcn_readfirstlane(listed ? d.set % a.Hkv : i);
@@ -436,8 +458,8 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(D, NT)) void k_cache_to
   for (; left > 0; first = false) {
     const Span sp = make_span(a, b, 0, rows);
     const int count = __builtin_amdgcn_readfirstlane(listed ? sa.counts[b * a.Hkv + g] : sp.count);
-    const int units = list_units(count, cost), last = split ? min(units, off + left) : units;
-    const int begin = max(off - cost, 0), end = max(last - cost, 0);
+    const int units = list_units(count, cost, fill), last = split ? min(units, off + left) : units;
+    const int begin = max(off - cost, 0), end = min(max(last - cost, 0), count);
 
     // this lane's query rows, and its part of Q as the B operand
     QueryRegs<D> qf[NT];
@@ -661,7 +683,11 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(D, NT)) void k_cache_to
 
     // the waves' states of a row joined, then the rows or a partial result stored
     const bool whole = off == 0 && last == units;
-    const size_t slot = 2 * (size_t)blockIdx.x + (first ? 0 : 1);
+    const int slot = 2 * (int)blockIdx.x + (first ? 0 : 1);
+    if (split && threadIdx.x == 0) {
+      if (off == 0) sa.where[b * a.Hkv + g].x = slot;
+      if (last == units) sa.where[b * a.Hkv + g].y = slot;
+    }
     const int tid = thread_here(), en = tid & 15, eq4 = tid >> 4 & 3, ew = tid >> 6;
     float* jo = (float*)lds;              // [wave][16][OP]
     float* jml = jo + kWaves * 16 * OP;   // [wave][16][2]
@@ -699,10 +725,10 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(D, NT)) void k_cache_to
         } else {
 #pragma unroll
           for (int e = 0; e < EPT; e += 4)
-            *(f32x4*)(sa.part + (slot * rows + r) * D + d0 + e) = f32x4{acc[e], acc[e + 1], acc[e + 2], acc[e + 3]};
+            *(f32x4*)(sa.part + ((size_t)slot * rows + r) * D + d0 + e) = f32x4{acc[e], acc[e + 1], acc[e + 2], acc[e + 3]};
           if (d0 == 0) {
-            sa.ml[(slot * rows + r) * 2] = top;
-            sa.ml[(slot * rows + r) * 2 + 1] = den;
+            sa.ml[((size_t)slot * rows + r) * 2] = top;
+            sa.ml[((size_t)slot * rows + r) * 2 + 1] = den;
           }
         }
       }
@@ -732,14 +758,11 @@ __global__ __launch_bounds__(64 * kWaves) void k_cache_join(CacheArgs a, SplitAr
   __shared__ float ldsl[PG], ldsm[PG];
   const int rows = a.S_q * a.G, b = blockIdx.x / a.Hkv, g = blockIdx.x % a.Hkv, r = blockIdx.y;
   const Span sp = make_span(a, b, 0, rows);
-  const bool listed = sa.counts != nullptr;
-  const int count = listed ? sa.counts[blockIdx.x] : sp.count;
+  const int count = sa.counts != nullptr ? sa.counts[blockIdx.x] : sp.count;
   if (count == 0) return;  // uniform over the workgroup
-  const Deal d = make_deal(a, sa, rows, (int*)lds, listed ? blockIdx.x : b);
-  const int units = list_units(count, d.cost), lo = d.before + (listed ? 0 : g * units);
-  const int w0 = lo / d.unit, w1 = (lo + units - 1) / d.unit;
+  const int2 at = sa.where[blockIdx.x];
+  const int first = at.x, w0 = at.x / 2, w1 = at.y / 2;
   if (w0 == w1) return;  // stored by its workgroup
-  const int first = 2 * w0 + (lo == w0 * d.unit ? 0 : 1);
   const int c = threadIdx.x % C, pg = threadIdx.x / C;
   auto slot_of = [&](int i) { return ((size_t)(i == 0 ? first : 2 * (w0 + i)) * rows + r); };
   const int parts = w1 - w0 + 1;
@@ -753,10 +776,10 @@ __global__ __launch_bounds__(64 * kWaves) void k_cache_join(CacheArgs a, SplitAr
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
   float l = 0.f;
   for (int i = pg; i < parts; i += PG) {
-    const size_t at = slot_of(i);
-    const float f = __builtin_amdgcn_exp2f(sa.ml[at * 2] - ms);
-    l += f * sa.ml[at * 2 + 1];
-    acc += f * *(const f32x4*)(sa.part + at * D + 4 * c);
+    const size_t s = slot_of(i);
+    const float f = __builtin_amdgcn_exp2f(sa.ml[s * 2] - ms);
+    l += f * sa.ml[s * 2 + 1];
+    acc += f * *(const f32x4*)(sa.part + s * D + 4 * c);
   }
   lds[pg][c] = acc;
   if (c == 0) ldsl[pg] = l;
@@ -1116,7 +1139,7 @@ ChunkPlan chunk_plan(int B, int Hkv, int rows, int D, int M) {
   p.grid = (int)(items * p.ns);
   const size_t slots = (size_t)p.grid * kTile;
   p.part = (slots * 2 * sizeof(float) + 255) & ~(size_t)255;
-  p.total = p.ns > 1 ? p.part + slots * D * sizeof(float) : 256;
+  p.total = p.ns > 1 ? p.part + slots * D * sizeof(float) : 0;
   return p;
 }
 
@@ -1164,7 +1187,7 @@ __global__ __launch_bounds__(256) void k_cache_lists(CacheArgs a, int rows, int2
 struct TokenPlan {
   int groups;  // workgroups
   bool split;
-  size_t part, list, counts, total;  // workspace offsets and size in bytes; {m, l} stand first
+  size_t part, where, list, counts, total;  // workspace offsets and size in bytes; {m, l} stand first
 };
 
 TokenPlan token_plan(int B, int Hkv, int rows, int D, int M) {
@@ -1176,10 +1199,12 @@ TokenPlan token_plan(int B, int Hkv, int rows, int D, int M) {
   p.split = M > 16;
   if (!p.split) p.groups = (int)lists;
   const size_t slots = 2 * (size_t)p.groups * rows;
-  p.part = (slots * 2 * sizeof(float) + 255) & ~(size_t)255;
-  p.list = p.part + slots * D * sizeof(float);
-  p.counts = p.list + (size_t)most * sizeof(int2);
-  p.total = p.split ? p.counts + (size_t)lists * sizeof(int) : 256;
+  auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
+  p.part = up(slots * 2 * sizeof(float));
+  p.where = p.part + up(slots * D * sizeof(float));
+  p.list = p.where + up((size_t)lists * sizeof(int2));
+  p.counts = p.list + up((size_t)most * sizeof(int2));
+  p.total = p.split ? p.counts + (size_t)lists * sizeof(int) : 0;
   return p;
 }
 
@@ -1190,6 +1215,7 @@ void launch_token(const CacheArgs& a, const TokenPlan& p, char* ws, int rows, hi
   if (p.split) {
     sa.ml = (float*)ws;
     sa.part = (float*)(ws + p.part);
+    sa.where = (int2*)(ws + p.where);
     if (a.mask != nullptr) {
       sa.list = (const int2*)(ws + p.list);
       sa.counts = (const int*)(ws + p.counts);

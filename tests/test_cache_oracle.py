@@ -121,8 +121,9 @@ def attn(**kw):
     (dict(q=None), 1, "non-NULL"), (dict(out=FAKE + 8), 1, "aligned"), (dict(Hq=6), 1, "multiple"),
     (dict(scale=0.0), 1, "scale"), (dict(scale=float("nan")), 1, "scale"), (dict(causal=2), 1, "causal"),
     (dict(win=-1), 1, "window_blocks"), (dict(sink=1), 1, "needs a window"), (dict(flags=2), 1, "flags"),
-    (dict(D=32), 2, "D=32"), (dict(ws=None), 1, "workspace"), (dict(ws=FAKE + 16), 1, "256-byte"),
-    (dict(n=16), 1, "smaller"), (dict(st=(4096, 512, 4)), 1, "strides of q"),
+    (dict(D=32), 2, "D=32"), (dict(ws=None, M=64), 1, "workspace"),
+    (dict(ws=FAKE + 16, M=64), 1, "256-byte"),
+    (dict(n=256, M=64), 1, "smaller"), (dict(st=(4096, 512, 4)), 1, "strides of q"),
     (dict(B=1 << 20, Hq=1 << 10, Hkv=1, S=1 << 10), 2, "many"),
 ])
 def test_attention_refuses(kw, code, text):
@@ -134,7 +135,7 @@ def test_attention_workspace_of_bad_sizes_is_zero():
     lib = _lib.load()
     assert lib.steel_attn_cache_workspace_bytes(1, 3, 2, 1, 64, 4) == 0
     assert "multiple" in _lib.last_error()
-    assert lib.steel_attn_cache_workspace_bytes(1, 4, 2, 1, 64, 4) > 0
+    assert lib.steel_attn_cache_workspace_bytes(1, 4, 2, 1, 64, 4) == 256  # none is used
 
 
 def test_load_refuses():
