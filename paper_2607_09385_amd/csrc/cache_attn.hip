@@ -243,12 +243,14 @@ __device__ __forceinline__ f32x4 scores(const u32x4& k, uint32_t ks, const Query
 // from partial results; a workgroup leaves at most two of them, slot 2 w for the
 // first list it touches and 2 w + 1 for the last.
 //
-// Few lists (a quarter of the workgroups at most): U is a multiple of the waves and every
-// list is filled up to a multiple of U, so a workgroup has one list only.  Many: a list counts
-// `cost` units beyond its pages for what it takes besides (page numbers, Q, the first
-// page's latency, the joined states): up to 8, but no more than a quarter of what a
-// workgroup gets.  Left out, the workgroups with the shortest of 64 ragged sequences'
-// lists took 238,000 cycles where the mean was 123,000.
+// Few lists (a quarter of the workgroups at most) of few pages (32 a workgroup): U is a
+// multiple of the waves and every list is filled up to a multiple of U, so a workgroup has
+// one list only.  64 lists of 51 pages: 22.4 us against 25.5 as below, 8 of 512: 24.7 against
+// 29.3; but 128 of 512: 124 against 117, for the workgroups left without a unit.
+// Else a list counts `cost` units beyond its pages for what it takes besides (page
+// numbers, Q, the first page's latency, the joined states): up to 8, but no more than a
+// quarter of what a workgroup gets.  Left out, the workgroups with the shortest of 64
+// ragged sequences' lists took 238,000 cycles where the mean was 123,000.
 struct SplitArgs {
   int groups;     // workgroups of the attention kernel
   // With a page mask: the live pages of every list, found ahead by k_cache_lists, as {place
@@ -317,7 +319,7 @@ __device__ __forceinline__ Deal make_deal(const CacheArgs& a, const SplitArgs& s
     tl += lds[kWaves + w];
   }
   Deal d;
-  if (4 * tl <= sa.groups) {
+  if (4 * tl <= sa.groups && tp < 32 * sa.groups) {
     const int u = (tp + sa.groups - tl - 1) / (sa.groups - tl);  // the lists' last units fill at most tl more
     d.cost = 0;
     d.unit = d.fill = __builtin_amdgcn_readfirstlane(max((u + kWaves - 1) / kWaves * kWaves, kWaves));
@@ -757,38 +759,43 @@ __global__ __launch_bounds__(64 * kWaves) void k_cache_join(CacheArgs a, SplitAr
   __shared__ __attribute__((aligned(16))) f32x4 lds[PG][C];
   __shared__ float ldsl[PG], ldsm[PG];
   const int rows = a.S_q * a.G, b = blockIdx.x / a.Hkv, g = blockIdx.x % a.Hkv, r = blockIdx.y;
+  const int2 at = sa.where[blockIdx.x];  // asked for before it is known to be written
   const Span sp = make_span(a, b, 0, rows);
   const int count = sa.counts != nullptr ? sa.counts[blockIdx.x] : sp.count;
   if (count == 0) return;  // uniform over the workgroup
-  const int2 at = sa.where[blockIdx.x];
   const int first = at.x, w0 = at.x / 2, w1 = at.y / 2;
   if (w0 == w1) return;  // stored by its workgroup
   const int c = threadIdx.x % C, pg = threadIdx.x / C;
-  auto slot_of = [&](int i) { return ((size_t)(i == 0 ? first : 2 * (w0 + i)) * rows + r); };
   const int parts = w1 - w0 + 1;
-  float m = -INFINITY;
-  for (int i = pg; i < parts; i += PG) m = fmaxf(m, sa.ml[slot_of(i) * 2]);
-  if (c == 0) ldsm[pg] = m;
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < PG; ++i) m = fmaxf(m, ldsm[i]);
-  const float ms = m == -INFINITY ? 0.f : m;
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-  float l = 0.f;
+  float m = -INFINITY, l = 0.f;
   for (int i = pg; i < parts; i += PG) {
-    const size_t s = slot_of(i);
-    const float f = __builtin_amdgcn_exp2f(sa.ml[s * 2] - ms);
-    l += f * sa.ml[s * 2 + 1];
-    acc += f * *(const f32x4*)(sa.part + s * D + 4 * c);
+    const size_t s = (size_t)(i == 0 ? first : 2 * (w0 + i)) * rows + r;
+    const float ms = sa.ml[s * 2], ls = sa.ml[s * 2 + 1];
+    const f32x4 os = *(const f32x4*)(sa.part + s * D + 4 * c);
+    const float mnew = fmaxf(m, ms), f0 = __builtin_amdgcn_exp2f(m - finite_max(mnew)),
+                f1 = __builtin_amdgcn_exp2f(ms - finite_max(mnew));
+    l = l * f0 + f1 * ls;
+    acc = acc * f0 + f1 * os;
+    m = mnew;
   }
   lds[pg][c] = acc;
-  if (c == 0) ldsl[pg] = l;
+  if (c == 0) {
+    ldsm[pg] = m;
+    ldsl[pg] = l;
+  }
   __syncthreads();
   if (pg != 0) return;
 #pragma unroll
-  for (int i = 1; i < PG; ++i) {
-    acc += lds[i][c];
-    l += ldsl[i];
+  for (int i = 1; i < PG; ++i) m = fmaxf(m, ldsm[i]);
+  const float ms = finite_max(m);
+  acc = f32x4{0.f, 0.f, 0.f, 0.f};
+  l = 0.f;
+#pragma unroll
+  for (int i = 0; i < PG; ++i) {
+    const float f = __builtin_amdgcn_exp2f(ldsm[i] - ms);
+    l += f * ldsl[i];
+    acc += f * lds[i][c];
   }
   const float out[4] = {acc[0], acc[1], acc[2], acc[3]};
   store_row<4>(a, sp, D, b, g, r, 4 * c, out, ms, l);
@@ -1196,7 +1203,7 @@ TokenPlan token_plan(int B, int Hkv, int rows, int D, int M) {
   const long long want = (most + 3) / 4;
   const int most_groups = 256 * waves_per_simd(D, rows <= 16 ? 1 : 2);
   p.groups = (int)(want < most_groups ? want : most_groups);
-  p.split = M > 16;
+  p.split = M > 24;
   if (!p.split) p.groups = (int)lists;
   const size_t slots = 2 * (size_t)p.groups * rows;
   auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
