@@ -247,6 +247,10 @@ __device__ __forceinline__ f32x4 scores(const u32x4& k, uint32_t ks, const Query
 // multiple of the waves and every list is filled up to a multiple of U, so a workgroup has
 // one list only.  64 lists of 51 pages: 22.4 us against 25.5 as below, 8 of 512: 24.7 against
 // 29.3; but 128 of 512: 124 against 117, for the workgroups left without a unit.
+// Lists of nearly one length (the longest up to 9/8 of the mean) of which two or three a CU
+// fill all but a few CUs (448 .. 512, 736 .. 768): a workgroup each, nothing is joined.  512 of
+// 32 pages: 40.9 us against 46.0, of 128: 115.8 against 124.4; but 384 of 128 pages: 104
+// against 98, 576 of 128 with D = 64: 72 against 65.
 // Else a list counts `cost` units beyond its pages for what it takes besides (page
 // numbers, Q, the first page's latency, the joined states): up to 8, but no more than a
 // quarter of what a workgroup gets.  Left out, the workgroups with the shortest of 64
@@ -296,33 +300,40 @@ __device__ __forceinline__ Deal make_deal(const CacheArgs& a, const SplitArgs& s
   const int sets = deal_sets(a, sa), per = (sets + T - 1) / T, i0 = tid * per, i1 = min(i0 + per, sets);
   const int heads = sa.counts != nullptr ? 1 : a.Hkv;
   // pages and lists of the call
-  int pages = 0, lists = 0;
+  int pages = 0, lists = 0, longest = 0;
   for (int i = i0; i < i1; ++i) {
     const int n = set_pages(a, sa, i, rows);
     pages += n * heads;
     lists += n > 0 ? heads : 0;
+    longest = max(longest, n);
   }
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) {
     pages += __shfl_xor(pages, o);
     lists += __shfl_xor(lists, o);
+    longest = max(longest, __shfl_xor(longest, o));
   }
   if (lane == 0) {
     lds[wave] = pages;
     lds[kWaves + wave] = lists;
+    lds[2 * kWaves + wave] = longest;
   }
   __syncthreads();
-  int tp = 0, tl = 0;
+  int tp = 0, tl = 0, top = 0;
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) {
     tp += lds[w];
     tl += lds[kWaves + w];
+    top = max(top, lds[2 * kWaves + w]);
   }
   Deal d;
   if (4 * tl <= sa.groups && tp < 32 * sa.groups) {
     const int u = (tp + sa.groups - tl - 1) / (sa.groups - tl);  // the lists' last units fill at most tl more
     d.cost = 0;
     d.unit = d.fill = __builtin_amdgcn_readfirstlane(max((u + kWaves - 1) / kWaves * kWaves, kWaves));
+  } else if (tl > 256 && tl <= sa.groups && (tl + 32) / 256 * 256 >= tl && (long long)top * tl <= (long long)tp + tp / 8) {
+    d.cost = 0;
+    d.unit = d.fill = __builtin_amdgcn_readfirstlane(top);
   } else {
     d.cost = __builtin_amdgcn_readfirstlane(min(tp / sa.groups / 4, 8));
     d.fill = 1;
@@ -337,12 +348,12 @@ __device__ __forceinline__ Deal make_deal(const CacheArgs& a, const SplitArgs& s
     const int y = __shfl_up(inc, o);
     if (lane >= o) inc += y;
   }
-  if (lane == 63) lds[2 * kWaves + wave] = inc;
+  if (lane == 63) lds[3 * kWaves + wave] = inc;
   __syncthreads();
   int before = inc - units, total = 0;
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) {
-    const int y = lds[2 * kWaves + w];
+    const int y = lds[3 * kWaves + w];
     before += w < wave ? y : 0;
     total += y;
   }
@@ -352,16 +363,16 @@ __device__ __forceinline__ Deal make_deal(const CacheArgs& a, const SplitArgs& s
     for (int i = i0; i < i1; ++i) {
       const int n = list_units(set_pages(a, sa, i, rows), d.cost, d.fill) * heads;
       if (want < before + n) {
-        lds[3 * kWaves] = i;
-        lds[3 * kWaves + 1] = before;
+        lds[4 * kWaves] = i;
+        lds[4 * kWaves + 1] = before;
         break;
       }
       before += n;
     }
   }
   __syncthreads();
-  d.set = __builtin_amdgcn_readfirstlane(lds[3 * kWaves]);
-  d.before = __builtin_amdgcn_readfirstlane(lds[3 * kWaves + 1]);
+  d.set = __builtin_amdgcn_readfirstlane(lds[4 * kWaves]);
+  d.before = __builtin_amdgcn_readfirstlane(lds[4 * kWaves + 1]);
   __syncthreads();
   return d;
 }
@@ -1197,20 +1208,24 @@ struct TokenPlan {
   size_t part, where, list, counts, total;  // workspace offsets and size in bytes; {m, l} stand first
 };
 
-TokenPlan token_plan(int B, int Hkv, int rows, int D, int M) {
+// pages: what a list can have at most.  Up to 24 a list is one workgroup's: nothing to join and
+// no second launch.  One token at 4 / 16 / 24 / 32 pages, whole against split: 8 heads of 128
+// 6.8 / 10.9 / 13.6 / 16.4 us against 11.3 / 13.7 / 13.7 / 13.7, 64 sequences of 8 heads
+// 10.4 / 19.5 / 27.2 / 32.9 us against 15.6 / 30.1 / 37.9 / 43.2.
+TokenPlan token_plan(int B, int Hkv, int rows, int D, int M, int pages) {
   TokenPlan p{};
-  const long long lists = (long long)B * Hkv, most = lists * M;
-  const long long want = (most + 3) / 4;
+  const long long lists = (long long)B * Hkv;
+  const long long want = (lists * pages + 3) / 4;
   const int most_groups = 256 * waves_per_simd(D, rows <= 16 ? 1 : 2);
   p.groups = (int)(want < most_groups ? want : most_groups);
-  p.split = M > 24;
+  p.split = pages > 24;
   if (!p.split) p.groups = (int)lists;
   const size_t slots = 2 * (size_t)p.groups * rows;
   auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
   p.part = up(slots * 2 * sizeof(float));
   p.where = p.part + up(slots * D * sizeof(float));
   p.list = p.where + up((size_t)lists * sizeof(int2));
-  p.counts = p.list + up((size_t)most * sizeof(int2));
+  p.counts = p.list + up((size_t)lists * M * sizeof(int2));
   p.total = p.split ? p.counts + (size_t)lists * sizeof(int) : 0;
   return p;
 }
@@ -1238,13 +1253,15 @@ void launch_token(const CacheArgs& a, const TokenPlan& p, char* ws, int rows, hi
 
 size_t cache_attn_ws(int B, int Hq, int Hkv, int S_q, int D, int M) {
   const int rows = S_q * (Hq / Hkv);
-  return rows <= 32 ? token_plan(B, Hkv, rows, D, M).total : chunk_plan(B, Hkv, rows, D, M).total;
+  return rows <= 32 ? token_plan(B, Hkv, rows, D, M, M).total : chunk_plan(B, Hkv, rows, D, M).total;
 }
 
 hipError_t launch_cache_attn(const CacheArgs& a, int D, void* ws, hipStream_t s) {
   const int rows = a.S_q * a.G;
   if (rows <= 32) {
-    const TokenPlan p = token_plan(a.B, a.Hkv, rows, D, a.M);
+    // a window's pages: its own, the sinks', and one more where the queries begin inside a page
+    const long long most = a.win > 0 ? (long long)a.sink + a.win + (a.S_q + 62) / kBlk : a.M;
+    const TokenPlan p = token_plan(a.B, a.Hkv, rows, D, a.M, (int)(most < a.M ? most : a.M));
     if (D == 64) launch_token<64>(a, p, (char*)ws, rows, s);
     else launch_token<128>(a, p, (char*)ws, rows, s);
   } else {
