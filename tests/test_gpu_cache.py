@@ -405,6 +405,77 @@ def test_long_and_many(case):
     check_attention(name, pool, table, np.array(lens), q, D ** -0.5, out_dtype=torch.bfloat16, **kw)
 
 
+SHORT = [c for c in ATTN if c[4] * c[1] // c[2] <= 32]
+
+
+@pytest.mark.parametrize("case", SHORT, ids=[c[0] for c in SHORT])
+def test_short_sequences_in_a_wide_table(case):
+    """As test_attention, with room for more pages than one workgroup takes."""
+    name, Hq, H, D, S, lens, kw = case
+    rng = np.random.default_rng(zlib.crc32(name.encode()) + 1)
+    P = sum(-(-max(n, 0) // 64) for n in lens) + 2
+    pool, table = random_pool(rng, P, H, D), random_table(rng, lens, P, extra=40)
+    kw = {k: v for k, v in kw.items() if k not in ("window_blocks", "sink_blocks")}
+    check_attention(name, pool, table, np.array(lens), bf16(rng, (len(lens), Hq, S, D)), D ** -0.5, **kw)
+
+
+@pytest.mark.parametrize("name,B,Hq,H,D,S,lo,hi", [
+    ("one length", 57, 8, 8, 64, 1, 1900, 1900), ("nearly", 64, 16, 8, 128, 1, 1700, 1900),
+    ("not nearly", 64, 8, 8, 64, 1, 1200, 1900), ("drafts", 128, 8, 4, 64, 3, 1700, 1800),
+    ("too many", 100, 8, 8, 64, 1, 1700, 1700), ("three a unit", 95, 16, 8, 64, 2, 1800, 1801)])
+def test_many_sequences_of_nearly_one_length(name, B, Hq, H, D, S, lo, hi):
+    rng = np.random.default_rng(B)
+    lens = rng.integers(lo, hi + 1, B)
+    pool = random_pool(rng, 200, H, D, 122, 129)
+    table = rng.integers(0, 200, (B, 30)).astype(np.int32)
+    check_attention(name, pool, table, lens, bf16(rng, (B, Hq, S, D)), D ** -0.5)
+
+
+@pytest.mark.parametrize("S,D", [(1, 64), (1, 128), (4, 128)])
+def test_values_of_every_size_in_long_sequences(S, D):
+    """Their partial results joined: values of 2^-90 to 2^120 and weights far apart."""
+    rng = np.random.default_rng(D + S)
+    lens = np.array([4000, 130, 9000])
+    P = 210
+    pool, table = random_pool(rng, P, 2, D), random_table(rng, lens, P)
+    pool[..., 66 * D:] = rng.integers(37, 248, (P, 2, 2 * D))
+    q = bf16(rng, (3, 8, S, D))
+    check_attention("large", pool, table, lens, q, D ** -0.5)
+    pool[..., 66 * D:] = rng.integers(122, 129, (P, 2, 2 * D))
+    check_attention("sharp", pool, table, lens, q, 2.0)
+
+
+@pytest.mark.parametrize("S,D", [(1, 64), (1, 128), (4, 128)])
+def test_nan_in_a_long_sequence(S, D):
+    """A stored NaN, in whatever part of its list, makes exactly the rows that see it NaN."""
+    rng = np.random.default_rng(S + D)
+    lens = np.array([5000, 900])
+    pool, table = random_pool(rng, 100, 2, D, 122, 129), random_table(rng, lens, 100)
+    q = bf16(rng, (2, 8, S, D))
+    s = steel()
+    base, _ = s.attn_cache(gpu(q), gpu(pool), ints(table), ints(lens))
+    for w, tok in ((0, 3000), (1, 0), (1, 2500), (1, 4997), (0, 4999)):
+        bad = pool.copy()
+        at = 64 * D + 2 * D * w
+        bad[table[0, tok // 64], 1, at:at + 2 * D].reshape(64, D // 32)[tok % 64] = 255
+        bad[table[0, tok // 64], 1, 32 * D * w:32 * D * (w + 1)].reshape(64, D // 2)[tok % 64] = 0
+        got, lse = s.attn_cache(gpu(q), gpu(bad), ints(table), ints(lens))
+        sees = torch.arange(S, device=DEV) + lens[0] - S >= tok
+        assert torch.isnan(got[0, 4:][:, sees]).all() and torch.equal(got[0, 4:][:, ~sees], base[0, 4:][:, ~sees])
+        assert torch.equal(got[0, :4], base[0, :4]) and torch.equal(got[1], base[1])
+
+
+@pytest.mark.parametrize("win,sink", [(22, 1), (23, 1), (24, 0), (25, 0)])
+def test_windows_around_the_pages_of_a_workgroup(win, sink):
+    """Queries on both sides of a page's end see one page more together."""
+    rng = np.random.default_rng(win)
+    for S, lens in ((2, [64 * 40 + 1, 64 * 30]), (3, [64 * 33 + 2, 65]), (1, [64 * 40 + 1, 64 * 40])):
+        P = sum(-(-n // 64) for n in lens) + 2
+        pool, table = random_pool(rng, P, 2, 64, 122, 129), random_table(rng, lens, P)
+        check_attention("window", pool, table, np.array(lens), bf16(rng, (2, 8, S, 64)), 0.125,
+                        window_blocks=win, sink_blocks=sink)
+
+
 @pytest.mark.parametrize("S,D,keep", [(1, 128, 0.1), (2, 64, 0.3), (100, 128, 0.2)])
 def test_long_with_a_page_mask(S, D, keep):
     rng = np.random.default_rng(S)
