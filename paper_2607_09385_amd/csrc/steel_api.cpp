@@ -324,6 +324,9 @@ int fused_call(const steel::Problem& p, const void* q, const void* k, const void
 }
 
 // Sizes shared by the calls on the paged cache.
+// A launch has fewer than 2^32 threads in x: workgroups of 256.
+constexpr long long kMaxGroups = 1 << 24;
+
 int check_cache(int B, int Hkv, int S, int D, int max_pages, int n_pages) {
   if (B < 1 || Hkv < 1 || S < 1 || max_pages < 1 || n_pages < 1)
     return fail(STEEL_ERR_INVALID_ARGUMENT,
@@ -332,8 +335,16 @@ int check_cache(int B, int Hkv, int S, int D, int max_pages, int n_pages) {
   if (D != 64 && D != 128) return fail(STEEL_ERR_UNSUPPORTED, "D=%d not supported (64 or 128)", D);
   if (max_pages > (1 << 24))
     return fail(STEEL_ERR_UNSUPPORTED, "max_pages=%d exceeds 2^24", max_pages);
-  if ((long long)B * Hkv > INT32_MAX || (long long)B * Hkv * S > ((long long)1 << 34))
-    return fail(STEEL_ERR_UNSUPPORTED, "B * Hkv * S = %d * %d * %d is too large", B, Hkv, S);
+  if ((long long)B * Hkv >= kMaxGroups)
+    return fail(STEEL_ERR_UNSUPPORTED, "B * Hkv = %d * %d is too large (below 2^24)", B, Hkv);
+  return STEEL_OK;
+}
+
+// Vectors of a call that writes or reads them, D / 8 threads each.
+int check_vectors(int B, int Hkv, int S, int D) {
+  if ((long long)B * Hkv * S / (2048 / D) >= kMaxGroups - 1)
+    return fail(STEEL_ERR_UNSUPPORTED, "B * Hkv * S = %d * %d * %d is too large (below 2^35 / D)", B,
+                Hkv, S);
   return STEEL_OK;
 }
 
@@ -364,10 +375,10 @@ int check_pages(int B, int max_pages, int n_pages) {
   if (B < 1 || max_pages < 1 || n_pages < 1)
     return fail(STEEL_ERR_INVALID_ARGUMENT, "sizes must be >= 1 (B=%d max_pages=%d n_pages=%d)", B,
                 max_pages, n_pages);
-  if (B > (1 << 24) || max_pages > (1 << 24) || n_pages > steel::kMaxPages ||
+  if (B > (1 << 23) || max_pages > (1 << 24) || n_pages > steel::kMaxPages ||
       (long long)B * max_pages > INT32_MAX)
     return fail(STEEL_ERR_UNSUPPORTED,
-                "B=%d rows of max_pages=%d, n_pages=%d: too large (2^31 entries, 2^24 a row, %d pages)",
+                "B=%d rows of max_pages=%d, n_pages=%d: too large (2^23 rows, 2^31 entries, 2^24 a row, %d pages)",
                 B, max_pages, n_pages, steel::kMaxPages);
   return STEEL_OK;
 }
@@ -631,6 +642,7 @@ int steel_cache_append(const void* k, const void* v, long long k_sb, long long k
                        int n_pages, void* stream) {
   g_err.clear();
   int rc = check_cache(B, Hkv, S, D, max_pages, n_pages);
+  if (rc == STEEL_OK) rc = check_vectors(B, Hkv, S, D);
   if (rc != STEEL_OK) return rc;
   if (!k || !v || !pages || !page_table || !lens)
     return fail(STEEL_ERR_INVALID_ARGUMENT, "k, v, pages, page_table and lens must be non-NULL");
@@ -648,7 +660,8 @@ int steel_cache_load(const uint8_t* pages, const int32_t* page_table, const int3
                      const int32_t* start, void* k, void* v, int B, int Hkv, int S, int D,
                      int max_pages, int n_pages, void* stream) {
   g_err.clear();
-  const int rc = check_cache(B, Hkv, S, D, max_pages, n_pages);
+  int rc = check_cache(B, Hkv, S, D, max_pages, n_pages);
+  if (rc == STEEL_OK) rc = check_vectors(B, Hkv, S, D);
   if (rc != STEEL_OK) return rc;
   if (!k || !v || !pages || !page_table || !lens)
     return fail(STEEL_ERR_INVALID_ARGUMENT, "pages, page_table, lens, k and v must be non-NULL");
@@ -772,7 +785,7 @@ int steel_pages_copy(uint8_t* pages, const int32_t* src, const int32_t* dst, int
   if (rc != STEEL_OK) return rc;
   if (n < 1 || n_pages < 1)
     return fail(STEEL_ERR_INVALID_ARGUMENT, "n (%d) and n_pages (%d) must be >= 1", n, n_pages);
-  if ((long long)n * (long long)((page_bytes + 16383) / 16384) > INT32_MAX)
+  if ((long long)n * (long long)((page_bytes + 16383) / 16384) >= kMaxGroups)
     return fail(STEEL_ERR_UNSUPPORTED, "%d pages of %zu bytes in one call are too many", n, page_bytes);
   const hipError_t e = steel::launch_pages_copy(pages, (long long)(page_bytes * (size_t)n_pages),
                                                 (long long)page_bytes, layers, src, dst, n, n_pages,

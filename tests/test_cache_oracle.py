@@ -100,6 +100,7 @@ def append(**kw):
     (dict(st=(8192, 1024, 68, 8192, 1024, 64)), 1, "strides of k"),
     (dict(st=(8192, 1024, 64, 8192, -8, 64)), 1, "strides of v"),
     (dict(B=1 << 20, Hkv=1 << 10, S=1 << 10), 2, "too large"),
+    (dict(B=1 << 12, Hkv=1 << 8, S=1 << 8, D=128), 2, "too large"), (dict(B=1 << 24, Hkv=1, S=1), 2, "too large"),
 ])
 def test_append_refuses(kw, code, text):
     st, msg = append(**kw)
@@ -124,7 +125,8 @@ def attn(**kw):
     (dict(D=32), 2, "D=32"), (dict(ws=None, M=64), 1, "workspace"),
     (dict(ws=FAKE + 16, M=64), 1, "256-byte"),
     (dict(n=256, M=64), 1, "smaller"), (dict(st=(4096, 512, 4)), 1, "strides of q"),
-    (dict(B=1 << 20, Hq=1 << 10, Hkv=1, S=1 << 10), 2, "many"),
+    (dict(B=1 << 20, Hq=1 << 10, Hkv=1, S=1 << 10), 2, "many"), (dict(B=1 << 24, Hq=1, Hkv=1), 2, "too large"),
+    (dict(B=1 << 20, Hq=1 << 3, Hkv=1 << 3, M=1 << 10), 2, "too large"),
 ])
 def test_attention_refuses(kw, code, text):
     st, msg = attn(**kw)
@@ -143,6 +145,7 @@ def test_load_refuses():
     assert lib.steel_cache_load(FAKE, FAKE, FAKE, None, None, FAKE, 1, 1, 1, 64, 1, 1, None) == 1
     assert lib.steel_cache_load(FAKE, FAKE, FAKE, None, FAKE + 8, FAKE, 1, 1, 1, 64, 1, 1, None) == 1
     assert lib.steel_cache_load(FAKE, FAKE, FAKE, None, FAKE, FAKE, 1, 1, 1, 80, 1, 1, None) == 2
+    assert lib.steel_cache_load(FAKE, FAKE, FAKE, None, FAKE, FAKE, 1 << 10, 1 << 10, 1 << 9, 64, 1, 1, None) == 2
 
 
 def test_page_calls_refuse():
@@ -153,6 +156,7 @@ def test_page_calls_refuse():
     assert lib.steel_pages_fork(f, f, f, f, f, g, 1, 1, 4, 8, None) == 1 and "alias" in _lib.last_error()
     assert lib.steel_pages_fork(f, f, f, f, g, g, 0, 1, 4, 8, None) == 1
     assert lib.steel_pages_fork(f, f, f, f, g, g, 1, 1, 4, (1 << 22) + 1, None) == 2
+    assert lib.steel_pages_fork(f, f, f, f, g, g, 1, (1 << 23) + 1, 4, 8, None) == 2
     n = lib.steel_pages_workspace_bytes(8, 2)
     assert n > 0 and lib.steel_pages_workspace_bytes(0, 2) == 0
     assert lib.steel_pages_grow(f, f, f, f, f, f, None, 2, 4, 8, f, n, None) == 1
