@@ -31,7 +31,7 @@ COMMON = [
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     "-Wno-unused-command-line-argument",
 ]
-# Both attention sources keep the compiler's MFMA accumulators in VGPRs: the
+# The attention sources keep the compiler's MFMA accumulators in VGPRs: the
 # softmax reads the scores with VALU instructions (AGPR-resident scores would
 # cost a copy per element), and attn_ws.hip runs two waves per SIMD, whose
 # 256 registers each hold no AGPR file.

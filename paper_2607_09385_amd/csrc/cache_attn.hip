@@ -4,20 +4,25 @@
 // over the keys j that row r sees, with the online softmax (running maximum m,
 // running sum l in fp32) over pages of 64 tokens.
 //
-// Operands.  S^T = K Q^T and O^T = V^T P^T on 16x16x32 bf16 MFMAs, so a query
-// row is a column of every result and its m, l and rescaling stay in the lanes
-// l % 16 = row.  Lane (n = l % 16, q = l / 16) of the K operand takes D / 4
-// consecutive channels of token n: one 16-byte (D = 128) load of codes straight
-// into registers, with one scale byte, since any order of the channels will do as
-// long as Q has the same.  Two codes and the scale become two bf16 values in one
-// instruction, without rounding.  The scores arrive with tokens 4 q .. 4 q + 3 of
-// each 16 in a lane, which is what the P^T operand takes when the tokens of a
-// page are numbered in that order; V goes through LDS, where a transposing read
-// of 4-bit elements gives each lane 16 tokens of one channel in the same order.
-// V's scales differ from token to token, along the sum, so they go into the
-// weights: p_rj 2^e_jg is formed once per group of 32 channels (a power of two:
-// exact) and rounded to bf16, the precision of the MFMA's operands (2^-9 of each
-// weight, averaged over the keys); l adds the weights before that rounding.
+// Scores.  S^T = K Q^T on the scaled MFMAs, which take K's codes and scale bytes as they are
+// stored: no decoding, and K's values exactly.  They want Q in 8 bits at most, so a query is
+// the sum of two E4M3 parts with a scale of their own per 32 channels (QueryRegs), each a
+// product: 2 x 35 cycles for 16 tokens and D = 128, against 4 x 17 of bf16 MFMAs and the 16
+// conversions a lane that those would need.
+//
+// A query row is a column of every result and its m, l and rescaling stay in the lanes
+// l % 16 = row (32 in the kernel for chunks).  Any order of the channels will do for K as
+// long as Q has the same, so lane (n = l % 16, q = l / 16) takes 32 consecutive channels of token n:
+// one 16-byte load of codes straight into registers, with one scale byte.
+//
+// O^T += V^T P^T on bf16 MFMAs.  The scores arrive with tokens 4 q .. 4 q + 3 of each 16 in a
+// lane, which is what the P^T operand takes when the tokens of a page are numbered in that
+// order; V goes through LDS, where a transposing read of 4-bit elements gives each lane 16
+// tokens of one channel in the same order.  V's scales differ from token to token, along the
+// sum, so they go into the weights: p_rj 2^e_jg is formed once per group of 32 channels (an
+// addition to the exponents: exact), and the codes alone are turned into bf16.  Weights are
+// rounded to bf16, the precision of the MFMA's operands (2^-9 of each weight on average, 2^-8
+// at most); l adds them before that rounding.
 //
 // A page id outside the pool is a page without visible keys; keys behind the
 // sequence's length are never visible, whatever their bytes.
@@ -411,6 +416,15 @@ __device__ __forceinline__ void store_row(const CacheArgs& a, const Span& sp, in
 // Few rows per key/value head (S_q G <= 16 NT): every row in one tile.  A workgroup's
 // waves take every fourth page of a list, each with a state of its own, joined at
 // the list's (or the workgroup's) end.
+//
+// Bound by memory where there is much of it: the next page's V (to LDS) and K (to registers)
+// are on their way while a wave computes, 12 waves a CU, 104 KB.  16 sequences of 32768
+// tokens, 8 heads of 128 (570 MB): 115 us, 5.0 TB/s; a kernel that only reads these records in
+// this order reaches 5.8.  64 ragged sequences of up to 32768 (374 MB): 87 us, 4.3 TB/s, for
+// the lists that begin and end inside workgroups.  4 sequences of 8000 (35 MB): 14 us, bound by
+// a chain of latencies: lengths, page numbers, 11 pages a wave, the joined states.  A third
+// wave per SIMD is worth more than registers: 2 waves, 73 us against 68 for 64 sequences of
+// 4000 on average; 4 waves spill (150 us and more).  With NT = 2 two waves fit.
 template <int D, int NT>
 __global__ __launch_bounds__(64 * kWaves, waves_per_simd(D, NT)) void k_cache_token(CacheArgs a, SplitArgs sa) {
   using R = Record<D>;
@@ -763,7 +777,8 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(D, NT)) void k_cache_to
 
 // Lists that lie in more than one workgroup of k_cache_token: their partial results
 // joined.  One workgroup per list and row; 8 (D = 128) or 16 threads of a column of 4
-// channels share the parts.
+// channels share the parts, each in one pass with a running maximum.  Latency bound (slots,
+// then parts, then the exchange): 4.8 us, 3 us of a step's time behind the kernel above.
 template <int D>
 __global__ __launch_bounds__(64 * kWaves) void k_cache_join(CacheArgs a, SplitArgs sa) {
   constexpr int C = D / 4, PG = 64 * kWaves / C;
@@ -819,6 +834,15 @@ __global__ __launch_bounds__(64 * kWaves) void k_cache_join(CacheArgs a, SplitAr
 // workgroup (16 conversions and four 16-byte LDS writes a thread) and read
 // transposed, as the dense kernels do.  Both are one page ahead: K by copies, V's codes in
 // registers until the present page is done.
+//
+// Bound by the MFMAs and the exponentials between them: 1000 queries of 32 heads against 12000
+// keys of 8 heads of 128 (188 GFLOP) 209 us with the join, 900 TFLOP/s; a large bf16 matrix
+// product reaches 1256 on the same card.  Two workgroups per CU; K Q^T costs twice its MFMA
+// time for the two parts of Q and is still no dearer than in bf16 (64 cycles for 64
+// channels, twice, against 4 x 33), without conversions or LDS traffic of bf16 keys.
+// Segments (below) fill the chip where the tiles are few: 211 us against 309 without here.
+// Waves of 64 rows were no faster (D = 64: 152 against 157 us, but 159 against 130 with 12 heads) or
+// spilled (D = 128: 596).
 struct ChunkArgs {
   int tiles, ns;  // tiles of a (sequence, key/value head), segments of a tile's list
   float* part;    // O [unit][tile][ns][128][D] when ns > 1
@@ -828,7 +852,8 @@ struct ChunkArgs {
 constexpr int kTile = 128;
 
 // Workgroup -> (unit, tile, segment).  With a multiple of 8 units each keeps to one XCD,
-// whose L2 then holds its keys and values; a unit's heaviest tiles come first.
+// whose L2 then holds its keys and values (2048 queries of 32 heads, 4096 keys: 139 us against
+// 160; 512 queries, 16384 keys 171 against 174); a unit's heaviest tiles come first.
 __device__ __forceinline__ void chunk_item(const CacheArgs& a, const ChunkArgs& ca, int* unit, int* tile,
                                            int* seg) {
   const int per = ca.tiles * ca.ns, units = a.B * a.Hkv, i = blockIdx.x;
@@ -1116,7 +1141,8 @@ __global__ __launch_bounds__(256, 2) void k_cache_chunk(CacheArgs a, ChunkArgs c
     }
 }
 
-// The segments of a tile's rows joined: a thread per row and 4 channels.
+// The segments of a tile's rows joined: a thread per row and 4 channels.  Memory bound: 2 segments
+// of 32000 rows of 128 (41 MB with the bf16 output) 11 us, 3.8 TB/s.
 template <int D>
 __global__ __launch_bounds__(256) void k_cache_chunk_join(CacheArgs a, ChunkArgs ca) {
   constexpr int C = D / 4, RPW = 256 / C;  // rows of a workgroup
@@ -1151,8 +1177,8 @@ ChunkPlan chunk_plan(int B, int Hkv, int rows, int D, int M) {
   ChunkPlan p{};
   p.tiles = (rows + kTile - 1) / kTile;
   const long long items = (long long)B * Hkv * p.tiles;
-  long long ns = items >= 512 ? 1 : (512 + items - 1) / items;  // two workgroups per CU
-  const long long most = (M + 7) / 8;                          // 8 pages a segment at least
+  long long ns = (512 + items - 1) / items;  // two workgroups per CU
+  const long long most = (M + 7) / 8;        // 8 pages a segment at least
   p.ns = (int)(ns < most ? ns : most);
   p.grid = (int)(items * p.ns);
   const size_t slots = (size_t)p.grid * kTile;
@@ -1172,7 +1198,8 @@ void launch_chunk(const CacheArgs& a, const ChunkPlan& p, void* ws, hipStream_t 
 }
 
 // The live pages of every list, one workgroup each: the pages of the span that exist and
-// whose mask byte is set, in order.
+// whose mask byte is set, in order.  A tenth of 64 lists of 512: 4.7 us, latency bound, and the
+// attention 21.7; where k_cache_token skipped the others itself it took 49.
 __global__ __launch_bounds__(256) void k_cache_lists(CacheArgs a, int rows, int2* list, int* counts) {
   __shared__ int found[2][4];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = blockIdx.x, b = i / a.Hkv;
@@ -1251,14 +1278,20 @@ void launch_token(const CacheArgs& a, const TokenPlan& p, char* ws, int rows, hi
   if (p.split) hipLaunchKernelGGL(k_cache_join<D>, dim3(a.B * a.Hkv, rows), wg, 0, s, a, sa);
 }
 
+// Up to 32 rows of a key/value head go to k_cache_token, which streams pages past the rows; more to
+// k_cache_chunk, whose tiles of 128 share them.  32 rows, 8 sequences of 16000 tokens: 50 us against
+// 84 (D = 128), 36 against 61 (D = 64); one sequence 30 against 38.  More than 32 rows would take a
+// third tile of accumulators, which do not fit into registers beside two.
+constexpr int kTokenRows = 32;
+
 size_t cache_attn_ws(int B, int Hq, int Hkv, int S_q, int D, int M) {
   const int rows = S_q * (Hq / Hkv);
-  return rows <= 32 ? token_plan(B, Hkv, rows, D, M, M).total : chunk_plan(B, Hkv, rows, D, M).total;
+  return rows <= kTokenRows ? token_plan(B, Hkv, rows, D, M, M).total : chunk_plan(B, Hkv, rows, D, M).total;
 }
 
 hipError_t launch_cache_attn(const CacheArgs& a, int D, void* ws, hipStream_t s) {
   const int rows = a.S_q * a.G;
-  if (rows <= 32) {
+  if (rows <= kTokenRows) {
     // a window's pages: its own, the sinks', and one more where the queries begin inside a page
     const long long most = a.win > 0 ? (long long)a.sink + a.win + (a.S_q + 62) / kBlk : a.M;
     const TokenPlan p = token_plan(a.B, a.Hkv, rows, D, a.M, (int)(most < a.M ? most : a.M));

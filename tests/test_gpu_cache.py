@@ -781,6 +781,54 @@ def test_a_step_captured_into_a_graph():
     assert held[2].tolist() == [67, 135, 10]
 
 
+def test_reordering_and_compaction_captured_into_a_graph():
+    """Fork, compaction, read-back and attention (long lists under a mask, a chunk) as one graph,
+    replayed over states that are put back, with eager work between."""
+    s, H, D, B, P = steel(), 2, 64, 3, 200
+    rng = np.random.default_rng(3)
+    lens = np.array([3000, 64, 2100], np.int32)
+    pool, table = random_pool(rng, P, H, D, 122, 129), random_table(rng, lens, P)
+    refs = np.zeros(P, np.int32)
+    refs[table[table >= 0]] = 1
+    M = table.shape[1]
+    mask = gpu((rng.random((B, H, M)) < 0.6).astype(np.uint8))
+    q1, qc = gpu(bf16(rng, (B, 4, 1, D))), gpu(bf16(rng, (B, 4, 50, D)))
+    start = [gpu(pool), ints(table), ints(lens), ints(refs)]
+    parent = ints([2, 0, 2])
+
+    def step(st):
+        t, l = s.pages_fork(*st[1:], parent)
+        live = s.pages_compact(st[0], t, l, st[3])
+        k, v = s.cache_load(st[0], t, l, 100)
+        return (t, l, live, k, v, *s.attn_cache(q1, st[0], t, l, block_mask=mask),
+                *s.attn_cache(q1, st[0], t, l), *s.attn_cache(qc, st[0], t, l))
+
+    held = [x.clone() for x in start]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step([x.clone() for x in start])
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        outs = step(held)
+    for i, order in enumerate(([2, 0, 2], [1, 1, 0], [-1, 2, 2], [0, 1, 2])):
+        parent.copy_(ints(order))
+        for x, y in zip(held, start):
+            x.copy_(y)
+        q1.copy_(gpu(bf16(rng, q1.shape)))
+        graph.replay()
+        eager = [x.clone() for x in start]
+        want = step(eager)
+        torch.cuda.synchronize()
+        for a, b in zip(outs, want):
+            assert torch.equal(a, b), f"replay {i}"
+        live = int(outs[2])
+        assert torch.equal(held[3], eager[3]) and torch.equal(held[0][:live], eager[0][:live])
+        ref = kv.fork(table, lens, refs, order)
+        assert live == int((ref[2] > 0).sum())
+
+
 def test_two_graphs_and_streams_do_not_share_anything():
     """Two captured calls replayed at one time on two streams, and calls by `stream=`."""
     s, D = steel(), 128
