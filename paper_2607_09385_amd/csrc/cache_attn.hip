@@ -105,6 +105,27 @@ __device__ __forceinline__ float row_sum(float x) {
   return half_pair_sum(__uint_as_float(r[0]) + __uint_as_float(r[1]));
 }
 
+// Inclusive sum over the wave's lanes in order; maximum of x >= 0 over them in lane 63.
+__device__ __forceinline__ int wave_scan(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);  // the lanes 1, 2, 4, 8 before, in rows of 16
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // lane 15 of the row before, to rows 1 and 3
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // lane 31, to rows 2 and 3
+  return x;
+}
+__device__ __forceinline__ int wave_total(int x) { return __builtin_amdgcn_readlane(wave_scan(x), 63); }
+__device__ __forceinline__ int wave_top(int x) {
+  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false));
+  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false));
+  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false));
+  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false));
+  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false));
+  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false));
+  return __builtin_amdgcn_readlane(x, 63);
+}
+
 // The weights of tokens t and t + 1, NaN for those in the set that are no further than lim.
 __device__ __forceinline__ uint32_t poison_pair(uint32_t w, uint32_t set, int t, int lim) {
   if ((set >> t & 1) && t <= lim) w = (w & 0xffff0000u) | 0x7fc0u;
@@ -197,22 +218,28 @@ __device__ __forceinline__ int query_scale(const bf16x8 (&x)[2]) {
 }
 
 template <int D>
-__device__ __forceinline__ QueryRegs<D> load_query(const __bf16* q, bool real, int q4) {
-  QueryRegs<D> r;
-  bf16x8 x[2] = {bf16x8{}, bf16x8{}};
+struct QueryRows {
+  bf16x8 x[D / 32];  // channels 16 q4 .., and 64 + 16 q4 ..
+};
+template <int D>
+__device__ __forceinline__ QueryRows<D> load_query(const __bf16* q, bool real, int q4) {
+  QueryRows<D> r{};
   if (real) {
-    x[0] = *(const bf16x8*)(q + 16 * q4);
-    x[1] = *(const bf16x8*)(q + 16 * q4 + 8);
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) r.x[i] = *(const bf16x8*)(q + i / 2 * 64 + 16 * q4 + i % 2 * 8);
   }
+  return r;
+}
+
+template <int D>
+__device__ __forceinline__ QueryRegs<D> split_query(const QueryRows<D>& raw, int q4) {
+  QueryRegs<D> r;
+  const bf16x8 x[2] = {raw.x[0], raw.x[1]};
   int hi[8], lo[8];
   const int e0 = query_scale<16>(x);  // of channels 32 (q4 / 2) ..
   split16(x, __uint_as_float((uint32_t)(254 - e0) << 23), hi, lo);
   if constexpr (D == 128) {
-    bf16x8 y[2] = {bf16x8{}, bf16x8{}};
-    if (real) {
-      y[0] = *(const bf16x8*)(q + 64 + 16 * q4);
-      y[1] = *(const bf16x8*)(q + 64 + 16 * q4 + 8);
-    }
+    const bf16x8 y[2] = {raw.x[2], raw.x[3]};
     const int e1 = query_scale<16>(y);  // of channels 64 + 32 (q4 / 2) ..
     split16(y, __uint_as_float((uint32_t)(254 - e1) << 23), hi + 4, lo + 4);
     // lane group g gives the scale of channels 32 g ..: that of group 2 (g % 2)
@@ -278,8 +305,10 @@ struct Deal {
   int unit;    // units per workgroup
   int cost;    // units of a list beyond its pages, or
   int fill;    //   the unit that lists are filled up to (else 1)
-  int set;     // set of lists asked for
+  int set;     // set of lists of this workgroup's first unit
   int before;  // units before it
+  int pages;   // pages of each of its lists
+  bool empty;  // some list has no page
 };
 
 // Units of a list; a list's pages follow its `cost` first ones.
@@ -297,88 +326,53 @@ __device__ __forceinline__ int set_pages(const CacheArgs& a, const SplitArgs& sa
   return sa.counts != nullptr ? sa.counts[i] : make_span(a, i, 0, rows).count;
 }
 
-// The set of this workgroup's first unit.  Thread t counts the sets t per .. t per + per - 1, and
-// the one that has the answer leaves it in LDS.
-__device__ __forceinline__ Deal make_deal(const CacheArgs& a, const SplitArgs& sa, int rows, int* lds) {
-  constexpr int T = 64 * kWaves;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int sets = deal_sets(a, sa), per = (sets + T - 1) / T, i0 = tid * per, i1 = min(i0 + per, sets);
-  const int heads = sa.counts != nullptr ? 1 : a.Hkv;
-  // pages and lists of the call
-  int pages = 0, lists = 0, longest = 0;
-  for (int i = i0; i < i1; ++i) {
-    const int n = set_pages(a, sa, i, rows);
+// Every wave finds it by itself, lane by lane 64 sets at a time: no exchange, and where there
+// are no more sets than that one load.
+__device__ __forceinline__ Deal make_deal(const CacheArgs& a, const SplitArgs& sa, int rows) {
+  const int lane = threadIdx.x & 63, sets = deal_sets(a, sa), heads = sa.counts != nullptr ? 1 : a.Hkv;
+  const int n0 = lane < sets ? set_pages(a, sa, lane, rows) : 0;
+  auto pages_at = [&](int i) { return i < 64 ? n0 : i < sets ? set_pages(a, sa, i, rows) : 0; };
+  int pages = 0, lists = 0, longest = 0, present = 0;
+  for (int i = lane; i - lane < sets; i += 64) {
+    const int n = pages_at(i);
     pages += n * heads;
     lists += n > 0 ? heads : 0;
+    present += n > 0 ? 1 : 0;
     longest = max(longest, n);
   }
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) {
-    pages += __shfl_xor(pages, o);
-    lists += __shfl_xor(lists, o);
-    longest = max(longest, __shfl_xor(longest, o));
-  }
-  if (lane == 0) {
-    lds[wave] = pages;
-    lds[kWaves + wave] = lists;
-    lds[2 * kWaves + wave] = longest;
-  }
-  __syncthreads();
-  int tp = 0, tl = 0, top = 0;
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
-    tp += lds[w];
-    tl += lds[kWaves + w];
-    top = max(top, lds[2 * kWaves + w]);
-  }
+  const int tp = wave_total(pages), tl = wave_total(lists), top = wave_top(longest);
   Deal d;
+  d.empty = wave_total(present) < sets;
   if (4 * tl <= sa.groups && tp < 32 * sa.groups) {
     const int u = (tp + sa.groups - tl - 1) / (sa.groups - tl);  // the lists' last units fill at most tl more
     d.cost = 0;
-    d.unit = d.fill = __builtin_amdgcn_readfirstlane(max((u + kWaves - 1) / kWaves * kWaves, kWaves));
+    d.unit = d.fill = max((u + kWaves - 1) / kWaves * kWaves, kWaves);
   } else if (tl > 256 && tl <= sa.groups && (tl + 32) / 256 * 256 >= tl && (long long)top * tl <= (long long)tp + tp / 8) {
     d.cost = 0;
-    d.unit = d.fill = __builtin_amdgcn_readfirstlane(top);
+    d.unit = d.fill = top;
   } else {
-    d.cost = __builtin_amdgcn_readfirstlane(min(tp / sa.groups / 4, 8));
+    d.cost = min(tp / sa.groups / 4, 8);
     d.fill = 1;
-    d.unit = __builtin_amdgcn_readfirstlane(max((tp + d.cost * tl + sa.groups - 1) / sa.groups, kWaves));
+    d.unit = max((tp + d.cost * tl + sa.groups - 1) / sa.groups, kWaves);
   }
-  // units before this thread's sets
   int units = 0;
-  for (int i = i0; i < i1; ++i) units += list_units(set_pages(a, sa, i, rows), d.cost, d.fill) * heads;
-  int inc = units;
-#pragma unroll
-  for (int o = 1; o < 64; o *= 2) {
-    const int y = __shfl_up(inc, o);
-    if (lane >= o) inc += y;
-  }
-  if (lane == 63) lds[3 * kWaves + wave] = inc;
-  __syncthreads();
-  int before = inc - units, total = 0;
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
-    const int y = lds[3 * kWaves + w];
-    before += w < wave ? y : 0;
-    total += y;
-  }
-  d.total = __builtin_amdgcn_readfirstlane(total);
+  for (int i = lane; i - lane < sets; i += 64) units += list_units(pages_at(i), d.cost, d.fill) * heads;
+  d.total = wave_total(units);
+  d.set = d.before = d.pages = 0;
   const long long want = (long long)blockIdx.x * d.unit;
-  if (want >= before && want < before + units) {
-    for (int i = i0; i < i1; ++i) {
-      const int n = list_units(set_pages(a, sa, i, rows), d.cost, d.fill) * heads;
-      if (want < before + n) {
-        lds[4 * kWaves] = i;
-        lds[4 * kWaves + 1] = before;
-        break;
-      }
-      before += n;
+  if (want >= d.total) return d;
+  for (int i0 = 0, before = 0; i0 < sets; i0 += 64) {
+    const int n = pages_at(i0 + lane), u = list_units(n, d.cost, d.fill) * heads, upto = before + wave_scan(u);
+    const uint64_t behind = __builtin_amdgcn_ballot_w64(upto > want);
+    if (behind != 0) {
+      const int l = __builtin_ctzll(behind);
+      d.set = i0 + l;
+      d.before = __builtin_amdgcn_readlane(upto - u, l);
+      d.pages = __builtin_amdgcn_readlane(n, l);
+      break;
     }
+    before = __builtin_amdgcn_readlane(upto, 63);
   }
-  __syncthreads();
-  d.set = __builtin_amdgcn_readfirstlane(lds[4 * kWaves]);
-  d.before = __builtin_amdgcn_readfirstlane(lds[4 * kWaves + 1]);
-  __syncthreads();
   return d;
 }
 
@@ -452,14 +446,14 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(D, NT)) void k_cache_to
     off = 0;
     left = 1;  // one list, whatever its length
   } else {
-    const Deal d = make_deal(a, sa, rows, (int*)lds);
+    const Deal d = make_deal(a, sa, rows);
     const long long lo = (long long)blockIdx.x * d.unit;
-    left = __builtin_amdgcn_readfirstlane((int)max(min((long long)d.unit, d.total - lo), 0ll));
+    left = (int)max(min((long long)d.unit, d.total - lo), 0ll);
     cost = d.cost;
     fill = d.fill;
     b = g = off = 0;
     if (left > 0) {
-      const int n = list_units(set_pages(a, sa, d.set, rows), cost, fill), at = (int)lo - d.before;
+      const int n = list_units(d.pages, cost, fill), at = (int)lo - d.before;
       const int i = at / n;  // list of the set
       b = __builtin_amdgcn_readfirstlane(listed ? d.set / a.Hkv : d.set);
       g = __builtin_amdgcn_readfirstlane(listed ? d.set % a.Hkv : i);
@@ -467,7 +461,7 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(D, NT)) void k_cache_to
     }
     // lists without a page: their rows are zero
     const int sets = deal_sets(a, sa), heads = listed ? 1 : a.Hkv;
-    for (int z = blockIdx.x; z < sets; z += sa.groups) {
+    for (int z = d.empty ? (int)blockIdx.x : sets; z < sets; z += sa.groups) {
       if (set_pages(a, sa, z, rows) > 0) continue;
       const int zb = listed ? z / a.Hkv : z, zg = listed ? z % a.Hkv : 0;
       const Span sp = make_span(a, zb, 0, rows);
@@ -487,27 +481,6 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(D, NT)) void k_cache_to
     const int count = __builtin_amdgcn_readfirstlane(listed ? sa.counts[b * a.Hkv + g] : sp.count);
     const int units = list_units(count, cost, fill), last = split ? min(units, off + left) : units;
     const int begin = max(off - cost, 0), end = min(max(last - cost, 0), count);
-
-    // this lane's query rows, and its part of Q as the B operand
-    QueryRegs<D> qf[NT];
-    int pos[NT];
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-      const int row = 16 * t + n, qi = row / a.G;
-      const bool real = row < rows && qi < sp.n;
-      pos[t] = real ? sp.first + qi : -1;
-      qf[t] = load_query<D>(a.q + b * a.q_sb + (g * a.G + row % a.G) * a.q_sh + qi * a.q_ss, real, q4);
-    }
-
-    f32x4 o[NT][CT];
-    float m[NT], l[NT];
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-#pragma unroll
-      for (int c = 0; c < CT; ++c) o[t][c] = f32x4{0.f, 0.f, 0.f, 0.f};
-      m[t] = -INFINITY;
-      l[t] = 0.f;
-    }
 
     // this wave's next 64 pages, one per lane: number (-1: no key of it is visible) and place
     int ids = -1, places = 0, base = begin + wave;
@@ -555,13 +528,34 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(D, NT)) void k_cache_to
         copy16_to_lds(rec + j * 1024, v_at, wv_lds + buf * kVBytes + j * 1024);
     };
 
+    // page numbers and query rows asked for together, then the first page, then Q is split
     int id = -1, buf = 0, kb_next = 0;
+    if (base < end) load_ids(base);
+    QueryRows<D> raw[NT];
+    int pos[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      const int row = 16 * t + n, qi = row / a.G;
+      const bool real = row < rows && qi < sp.n;
+      pos[t] = real ? sp.first + qi : -1;
+      raw[t] = load_query<D>(a.q + b * a.q_sb + (g * a.G + row % a.G) * a.q_sh + qi * a.q_ss, real, q4);
+    }
     if (base < end) {
-      load_ids(base);
       id = __builtin_amdgcn_readfirstlane(ids);
       kb_next = __builtin_amdgcn_readfirstlane(places);
       copy_v(record(max(id, 0)), 0);
       load_k(record(max(id, 0)));
+    }
+    QueryRegs<D> qf[NT];  // the lane's part of Q as the B operand
+    f32x4 o[NT][CT];
+    float m[NT], l[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      qf[t] = split_query<D>(raw[t], q4);
+#pragma unroll
+      for (int c = 0; c < CT; ++c) o[t][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+      m[t] = -INFINITY;
+      l[t] = 0.f;
     }
     for (int i = base; i < end; i += kWaves, buf ^= 1) {
       const bool there = id >= 0;  // else page 0 stands in, none of its keys visible
