@@ -26,14 +26,15 @@ from . import STEEL_OUT_BF16, _check_bf16_rows, _on, _torch
 
 def _ints(name, t, shape, device):
     torch = _torch()
+    if isinstance(t, torch.Tensor) and t.dtype is torch.int32 and t.shape == shape \
+            and t.device == device and t.is_contiguous():
+        return t.data_ptr()
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
-    if t.dtype != torch.int32 or t.shape != shape or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous int32 tensor {list(shape)} "
-                         f"(got {t.dtype} {tuple(t.shape)})")
     if t.device != device:
         raise ValueError(f"{name} must be on {device} (got {t.device})")
-    return t.data_ptr()
+    raise ValueError(f"{name} must be a contiguous int32 tensor {list(shape)} "
+                     f"(got {t.dtype} {tuple(t.shape)})")
 
 
 def _numel(name, t):
@@ -242,7 +243,8 @@ def pages_grow(page_table, lens, refs, new, *, stream=None):
     nbytes = _bytes("steel_pages_workspace_bytes", n_pages, B)
     i32 = page_table.dtype
     n = nbytes // 4
-    ws, src, dst, left = _empty(stream, page_table, ((n + 2 * B + 1,), i32))[0].split((n, B, B, 1))
+    made, = _empty(stream, page_table, ((n + 2 * B + 1,), i32))
+    ws, src, dst, left = made.split_with_sizes((n, B, B, 1))
     _call(_lib.load().steel_pages_grow, device, stream, tp, lp, rp, np_, src.data_ptr(),
           dst.data_ptr(), left.data_ptr(), B, M, n_pages, ws.data_ptr(), nbytes)
     return src, dst, left
@@ -267,7 +269,8 @@ def pages_compact(pages, page_table, lens, refs, *, stream=None):
     rp = _ints("refs", refs, (n_pages,), device)
     nbytes = _bytes("steel_pages_workspace_bytes", n_pages, B)
     i32 = page_table.dtype
-    ws, live = _empty(stream, pages, ((nbytes // 4 + 1,), i32))[0].split((nbytes // 4, 1))
+    made, = _empty(stream, pages, ((nbytes // 4 + 1,), i32))
+    ws, live = made.split_with_sizes((nbytes // 4, 1))
     _call(_lib.load().steel_pages_compact, device, stream, pages.data_ptr(), tp, lp, rp,
           live.data_ptr(), B, M, layers, n_pages, page_bytes, ws.data_ptr(), nbytes)
     return live

@@ -756,15 +756,22 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(D, NT)) void k_cache_to
     }
     __syncthreads();
 
-    if (!split) break;
-    left -= last - off;
+    left = split ? left - (last - off) : 0;
+    if (left == 0) break;
+    // the next list that has a page
     off = 0;
-    do {  // the next list that has a page
-      if (++g == a.Hkv) {
-        g = 0;
-        ++b;
-      }
-    } while (b < a.B && (listed ? sa.counts[b * a.Hkv + g] == 0 : g == 0 && make_span(a, b, 0, rows).count == 0));
+    if (listed) {
+      do {
+        if (++g == a.Hkv) {
+          g = 0;
+          ++b;
+        }
+      } while (b < a.B && sa.counts[b * a.Hkv + g] == 0);
+    } else if (++g == a.Hkv) {
+      g = 0;
+      do ++b;
+      while (b < a.B && make_span(a, b, 0, rows).count == 0);
+    }
     if (b >= a.B) break;
   }
 }
