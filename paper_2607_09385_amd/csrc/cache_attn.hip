@@ -284,8 +284,8 @@ __device__ __forceinline__ f32x4 scores(const u32x4& k, uint32_t ks, const Query
 // 32 pages: 40.9 us against 46.0, of 128: 115.8 against 124.4; but 384 of 128 pages: 104
 // against 98, 576 of 128 with D = 64: 72 against 65.
 // Else a list counts `cost` units beyond its pages for what it takes besides (page
-// numbers, Q, the first page's latency, the joined states): up to 8, but no more than a
-// quarter of what a workgroup gets.  Left out, the workgroups with the shortest of 64
+// numbers, Q, the first page's latency, the joined states): up to 10, but no more than a
+// quarter of what a workgroup gets (64 ragged sequences 82.6 us, with 8 85.2, with 12 83.5).  Left out, the workgroups with the shortest of 64
 // ragged sequences' lists took 238,000 cycles where the mean was 123,000.
 struct SplitArgs {
   int groups;     // workgroups of the attention kernel
@@ -351,7 +351,7 @@ __device__ __forceinline__ Deal make_deal(const CacheArgs& a, const SplitArgs& s
     d.cost = 0;
     d.unit = d.fill = top;
   } else {
-    d.cost = min(tp / sa.groups / 4, 8);
+    d.cost = min(tp / sa.groups / 4, 10);
     d.fill = 1;
     d.unit = max((tp + d.cost * tl + sa.groups - 1) / sa.groups, kWaves);
   }
@@ -845,12 +845,18 @@ __global__ __launch_bounds__(64 * kWaves) void k_cache_join(CacheArgs a, SplitAr
 // Waves of 64 rows were no faster (D = 64: 152 against 157 us, but 159 against 130 with 12 heads) or
 // spilled (D = 128: 596).
 struct ChunkArgs {
-  int tiles, ns;  // tiles of a (sequence, key/value head), segments of a tile's list
+  int tiles, ns;  // tiles of a (sequence, key/value head), segments of a tile's list at most
+  int least;      // pages of a segment at least
   float* part;    // O [unit][tile][ns][128][D] when ns > 1
   float* ml;      // {m, l}
 };
 
 constexpr int kTile = 128;
+
+// Segments of a tile with `count` pages.
+__device__ __forceinline__ int tile_segments(const ChunkArgs& ca, int count) {
+  return min(ca.ns, max(count / ca.least, 1));
+}
 
 // Workgroup -> (unit, tile, segment).  With a multiple of 8 units each keeps to one XCD,
 // whose L2 then holds its keys and values (2048 queries of 32 heads, 4096 keys: 139 us against
@@ -889,7 +895,9 @@ __global__ __launch_bounds__(256, 2) void k_cache_chunk(CacheArgs a, ChunkArgs c
   const int n = lane & 31, hf = lane >> 5;
   const int r0 = tile * kTile, r1 = min(r0 + kTile, rows);
   const Span sp = make_span(a, b, r0, r1);
-  const int p0 = (int)((long long)sp.count * seg / ca.ns), p1 = (int)((long long)sp.count * (seg + 1) / ca.ns);
+  const int ns = tile_segments(ca, sp.count);
+  if (seg >= ns) return;
+  const int p0 = (int)((long long)sp.count * seg / ns), p1 = (int)((long long)sp.count * (seg + 1) / ns);
 
   // this lane's row
   const int row = r0 + 32 * wave + n, qi = row / a.G;
@@ -1119,7 +1127,7 @@ __global__ __launch_bounds__(256, 2) void k_cache_chunk(CacheArgs a, ChunkArgs c
   // this lane's row: channels 32 d + 8 i + 4 hf ..
   const float ls = half_pair_sum(l);
   if (row >= r1) return;
-  if (ca.ns > 1) {
+  if (ns > 1) {
     const size_t at = (((size_t)unit * ca.tiles + tile) * ca.ns + seg) * kTile + 32 * wave + n;
 #pragma unroll
     for (int d = 0; d < DT; ++d)
@@ -1152,14 +1160,16 @@ __global__ __launch_bounds__(256) void k_cache_chunk_join(CacheArgs a, ChunkArgs
   const int d0 = threadIdx.x % C * 4, unit = (int)(i / rows), r = (int)(i % rows);
   if (unit >= a.B * a.Hkv) return;
   const int b = unit / a.Hkv, g = unit % a.Hkv, tile = r / kTile;
-  const Span sp = make_span(a, b, 0, rows);
+  const Span sp = make_span(a, b, tile * kTile, min((tile + 1) * kTile, rows));
+  const int ns = tile_segments(ca, sp.count);
+  if (ns == 1) return;  // stored by its workgroup
   const size_t at = ((size_t)unit * ca.tiles + tile) * ca.ns * kTile + r % kTile;
   float top = -INFINITY;
-  for (int s = 0; s < ca.ns; ++s) top = fmaxf(top, ca.ml[(at + (size_t)s * kTile) * 2]);
+  for (int s = 0; s < ns; ++s) top = fmaxf(top, ca.ml[(at + (size_t)s * kTile) * 2]);
   const float ts = top == -INFINITY ? 0.f : top;
   float den = 0.f;
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-  for (int s = 0; s < ca.ns; ++s) {
+  for (int s = 0; s < ns; ++s) {
     const size_t p = at + (size_t)s * kTile;
     const float f = __builtin_amdgcn_exp2f(ca.ml[p * 2] - ts);
     den += f * ca.ml[p * 2 + 1];
@@ -1170,16 +1180,20 @@ __global__ __launch_bounds__(256) void k_cache_chunk_join(CacheArgs a, ChunkArgs
 }
 
 struct ChunkPlan {
-  int tiles, ns, grid;
+  int tiles, ns, least, grid;
   size_t part, total;
 };
 
-ChunkPlan chunk_plan(int B, int Hkv, int rows, int D, int M) {
+ChunkPlan chunk_plan(int B, int Hkv, int rows, int D, int pages) {
   ChunkPlan p{};
   p.tiles = (rows + kTile - 1) / kTile;
   const long long items = (long long)B * Hkv * p.tiles;
   long long ns = (512 + items - 1) / items;  // two workgroups per CU
-  const long long most = (M + 7) / 8;        // 8 pages a segment at least
+  // A segment saves its share of a tile's pages and costs 64 KB or 128 KB written and read back, the
+  // more the more tiles do so: 8 pages at least, 27 with 384 tiles.  With 8 always, 384 tiles of 10
+  // pages took 49 us (31), 376 of up to 36 82 us (71), 256 of 9 30 us (19).
+  p.least = 8 + (int)(items < 512 ? items / 20 : 0);
+  const long long most = pages / p.least > 1 ? pages / p.least : 1;
   p.ns = (int)(ns < most ? ns : most);
   p.grid = (int)(items * p.ns);
   const size_t slots = (size_t)p.grid * kTile;
@@ -1190,7 +1204,7 @@ ChunkPlan chunk_plan(int B, int Hkv, int rows, int D, int M) {
 
 template <int D>
 void launch_chunk(const CacheArgs& a, const ChunkPlan& p, void* ws, hipStream_t s) {
-  ChunkArgs ca{p.tiles, p.ns, (float*)((char*)ws + p.part), (float*)ws};
+  ChunkArgs ca{p.tiles, p.ns, p.least, (float*)((char*)ws + p.part), (float*)ws};
   hipLaunchKernelGGL(k_cache_chunk<D>, dim3(p.grid), dim3(256), 0, s, a, ca);
   if (p.ns > 1) {
     const long long rows = (long long)a.B * a.Hkv * a.S_q * a.G;
@@ -1290,16 +1304,21 @@ size_t cache_attn_ws(int B, int Hq, int Hkv, int S_q, int D, int M) {
   return rows <= kTokenRows ? token_plan(B, Hkv, rows, D, M, M).total : chunk_plan(B, Hkv, rows, D, M).total;
 }
 
+// Pages that `queries` of a sequence next to each other can see: with a window its own, the
+// sinks', and more where the queries lie in several pages.
+int most_pages(const CacheArgs& a, int queries) {
+  const long long n = a.win > 0 ? (long long)a.sink + a.win + (queries + 62) / kBlk : a.M;
+  return (int)(n < a.M ? n : a.M);
+}
+
 hipError_t launch_cache_attn(const CacheArgs& a, int D, void* ws, hipStream_t s) {
   const int rows = a.S_q * a.G;
   if (rows <= kTokenRows) {
-    // a window's pages: its own, the sinks', and one more where the queries begin inside a page
-    const long long most = a.win > 0 ? (long long)a.sink + a.win + (a.S_q + 62) / kBlk : a.M;
-    const TokenPlan p = token_plan(a.B, a.Hkv, rows, D, a.M, (int)(most < a.M ? most : a.M));
+    const TokenPlan p = token_plan(a.B, a.Hkv, rows, D, a.M, most_pages(a, a.S_q));
     if (D == 64) launch_token<64>(a, p, (char*)ws, rows, s);
     else launch_token<128>(a, p, (char*)ws, rows, s);
   } else {
-    const ChunkPlan p = chunk_plan(a.B, a.Hkv, rows, D, a.M);
+    const ChunkPlan p = chunk_plan(a.B, a.Hkv, rows, D, most_pages(a, (kTile - 1) / a.G + 2));
     if (D == 64) launch_chunk<64>(a, p, ws, s);
     else launch_chunk<128>(a, p, ws, s);
   }

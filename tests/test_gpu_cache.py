@@ -476,6 +476,19 @@ def test_windows_around_the_pages_of_a_workgroup(win, sink):
                         window_blocks=win, sink_blocks=sink)
 
 
+@pytest.mark.parametrize("name,Hq,H,D,S,lens,kw", [
+    ("one segment and several", 8, 2, 64, 300, [300, 2000, 9000, 1100], {}),
+    ("wide table", 5, 1, 128, 100, [100, 6000], {"causal": False}),
+    ("window", 7, 1, 64, 200, [3000, 250], {"window_blocks": 30, "sink_blocks": 1}),
+    ("tiles of many heads", 32, 8, 128, 200, [1700, 210], {})])
+def test_tiles_of_unequal_lists(name, Hq, H, D, S, lens, kw):
+    """Tiles whose lists are and are not cut into segments, in one call."""
+    rng = np.random.default_rng(S + D)
+    P = sum(-(-n // 64) for n in lens) + 5
+    pool, table = random_pool(rng, P, H, D, 122, 129), random_table(rng, lens, P, extra=100)
+    check_attention(name, pool, table, np.array(lens), bf16(rng, (len(lens), Hq, S, D)), D ** -0.5, **kw)
+
+
 @pytest.mark.parametrize("S,D,keep", [(1, 128, 0.1), (2, 64, 0.3), (100, 128, 0.2)])
 def test_long_with_a_page_mask(S, D, keep):
     rng = np.random.default_rng(S)
