@@ -414,9 +414,9 @@ __device__ __forceinline__ void store_row(const CacheArgs& a, const Span& sp, in
 // Bound by memory where there is much of it: the next page's V (to LDS) and K (to registers)
 // are on their way while a wave computes, 12 waves a CU, 104 KB.  16 sequences of 32768
 // tokens, 8 heads of 128 (570 MB): 115 us, 5.0 TB/s; a kernel that only reads these records in
-// this order reaches 5.8.  64 ragged sequences of up to 32768 (374 MB): 87 us, 4.3 TB/s, for
-// the lists that begin and end inside workgroups.  4 sequences of 8000 (35 MB): 14 us, bound by
-// a chain of latencies: lengths, page numbers, 11 pages a wave, the joined states.  A third
+// this order reaches 5.8.  64 ragged sequences of up to 32768 (374 MB): 83 us, 4.5 TB/s, for
+// the lists that begin and end inside workgroups.  4 sequences of 8000 (35 MB): 12 us, bound by
+// a chain of latencies: lengths, page numbers, 2 pages a wave, the joined states.  A third
 // wave per SIMD is worth more than registers: 2 waves, 73 us against 68 for 64 sequences of
 // 4000 on average; 4 waves spill (150 us and more).  With NT = 2 two waves fit.
 template <int D, int NT>
@@ -837,8 +837,9 @@ __global__ __launch_bounds__(64 * kWaves) void k_cache_join(CacheArgs a, SplitAr
 // registers until the present page is done.
 //
 // Bound by the MFMAs and the exponentials between them: 1000 queries of 32 heads against 12000
-// keys of 8 heads of 128 (188 GFLOP) 209 us with the join, 900 TFLOP/s; a large bf16 matrix
-// product reaches 1256 on the same card.  Two workgroups per CU; K Q^T costs twice its MFMA
+// keys of 8 heads of 128 (188 GFLOP) 204 us with the join, 925 TFLOP/s; a large bf16 matrix
+// product reaches 1256 on the same card.  MFMAs take 38% of the cycles, VALU 43%, and the two
+// hardly overlap.  Two workgroups per CU; K Q^T costs twice its MFMA
 // time for the two parts of Q and is still no dearer than in bf16 (64 cycles for 64
 // channels, twice, against 4 x 33), without conversions or LDS traffic of bf16 keys.
 // Segments (below) fill the chip where the tiles are few: 211 us against 309 without here.
@@ -1214,7 +1215,7 @@ void launch_chunk(const CacheArgs& a, const ChunkPlan& p, void* ws, hipStream_t 
 
 // The live pages of every list, one workgroup each: the pages of the span that exist and
 // whose mask byte is set, in order.  A tenth of 64 lists of 512: 4.7 us, latency bound, and the
-// attention 21.7; where k_cache_token skipped the others itself it took 49.
+// attention 19.9; where k_cache_token skipped the others itself it took 49.
 __global__ __launch_bounds__(256) void k_cache_lists(CacheArgs a, int rows, int2* list, int* counts) {
   __shared__ int found[2][4];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = blockIdx.x, b = i / a.Hkv;
