@@ -126,11 +126,9 @@ __device__ __forceinline__ int wave_top(int x) {
   return __builtin_amdgcn_readlane(x, 63);
 }
 
-// The weights of tokens t and t + 1, NaN for those in the set that are no further than lim.
-__device__ __forceinline__ uint32_t poison_pair(uint32_t w, uint32_t set, int t, int lim) {
-  if ((set >> t & 1) && t <= lim) w = (w & 0xffff0000u) | 0x7fc0u;
-  if ((set >> (t + 1) & 1) && t + 1 <= lim) w = (w & 0xffffu) | 0x7fc00000u;
-  return w;
+// Whether a row that sees the keys 0 .. last of a page (last < 0: none) sees one of the set.
+__device__ __forceinline__ bool sees_any(uint64_t set, int last) {
+  return last >= 0 && (set & ((2ull << last) - 1)) != 0;
 }
 
 // A running maximum to subtract: 0 before the first key.
@@ -285,8 +283,9 @@ __device__ __forceinline__ f32x4 scores(const u32x4& k, uint32_t ks, const Query
 // against 98, 576 of 128 with D = 64: 72 against 65.
 // Else a list counts `cost` units beyond its pages for what it takes besides (page
 // numbers, Q, the first page's latency, the joined states): up to 10, but no more than a
-// quarter of what a workgroup gets (64 ragged sequences 82.6 us, with 8 85.2, with 12 83.5).  Left out, the workgroups with the shortest of 64
-// ragged sequences' lists took 238,000 cycles where the mean was 123,000.
+// quarter of what a workgroup gets (64 ragged sequences 82.6 us, with 8 85.2, with 12 83.5).
+// Left out, the workgroups with the shortest of 64 ragged sequences' lists took 238,000
+// cycles where the mean was 123,000.
 struct SplitArgs {
   int groups;     // workgroups of the attention kernel
   // With a page mask: the live pages of every list, found ahead by k_cache_lists, as {place
@@ -639,17 +638,6 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(D, NT)) void k_cache_to
           pk[nt][e] = pack_bf16(p0, p1);
         }
       }
-      if (v_nan != 0) {  // NaN for the weights of values that stand for NaN, where the row sees them
-        uint32_t set[2] = {(uint32_t)(v_nan >> (4 * q4)), (uint32_t)(v_nan >> (4 * q4) >> 32)};
-        asm volatile("" : "+v"(set[0]), "+v"(set[1]));  // tested where it is rarely needed
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          const int lim = there ? row_limit(a, sp, pos[nt], kb) - 4 * q4 : -1;
-#pragma unroll
-          for (int e = 0; e < 8; ++e)  // tokens 16 (e / 2) + 2 (e % 2) of the lane's group
-            pk[nt][e] = poison_pair(pk[nt][e], set[e / 4], 16 * (e / 2 % 2) + 2 * (e % 2), lim - 32 * (e / 4));
-        }
-      }
       // O^T += V^T P^T, 32 channels (one scale per token) at a time.  The scaling of P is an
       // addition to both exponents of a pair: P + (e - 127) in units of 2^7, not below 0.  A
       // weight under 2^-126 then ends as up to 2^(e - 254), 2^-127 of what the token's values
@@ -699,6 +687,14 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(D, NT)) void k_cache_to
             o[nt][ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, __builtin_bit_cast(bf16x8, u[nt][1]), o[nt][ct], 0, 0, 0);
           }
         }
+      }
+      if (v_nan != 0) {  // values that stand for NaN (as numbers above), where the row sees them
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+          if (there && sees_any(v_nan, row_limit(a, sp, pos[nt], kb))) {
+#pragma unroll
+            for (int c = 0; c < CT; ++c) o[nt][c] = f32x4{} + __builtin_nanf("");
+          }
       }
     }
 
@@ -1067,7 +1063,8 @@ __global__ __launch_bounds__(256, 2) void k_cache_chunk(CacheArgs a, ChunkArgs c
       for (int d = 0; d < DT; ++d) o[d] *= alpha;
     }
     const float ms = finite_max(m);
-    bf16x8 pa[2][2];
+    const uint32_t vb = vr_at + buf * VB;
+    // Weights of 16 tokens, then their products: the next 16's exponentials run beside these
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -1081,28 +1078,7 @@ __global__ __launch_bounds__(256, 2) void k_cache_chunk(CacheArgs a, ChunkArgs c
           l += w1;
           u[e] = pack_bf16(w0, w1);
         }
-        pa[t][c] = __builtin_bit_cast(bf16x8, u);
-      }
-    if (v_nan != 0) {  // NaN for the weights of values that stand for NaN, where the row sees them
-      const int lim = row_limit(a, sp, pos, kb) - 4 * hf;
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        uint32_t set = (uint32_t)(v_nan >> (32 * t)) >> (4 * hf);
-        asm volatile("" : "+v"(set));  // tested where it is rarely needed, not ahead of the loop
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          u32x4 u = __builtin_bit_cast(u32x4, pa[t][c]);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) u[e] = poison_pair(u[e], set, 16 * c + 8 * (e / 2) + 2 * (e % 2), lim - 32 * t);
-          pa[t][c] = __builtin_bit_cast(bf16x8, u);
-        }
-      }
-    }
-    const uint32_t vb = vr_at + buf * VB;
-#pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-      for (int c = 0; c < 2; ++c)
+        const bf16x8 pa = __builtin_bit_cast(bf16x8, u);
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
           const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
@@ -1110,8 +1086,13 @@ __global__ __launch_bounds__(256, 2) void k_cache_chunk(CacheArgs a, ChunkArgs c
           const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
               (lds_s16x4*)(lds_cp)((vb ^ (uint32_t)((d << 6) | 32)) + (32 * t + 16 * c + 8) * RB));
           const bf16x8 vf = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pa[t][c], o[d], 0, 0, 0);
+          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pa, o[d], 0, 0, 0);
         }
+      }
+    if (v_nan != 0 && sees_any(v_nan, row_limit(a, sp, pos, kb))) {  // values that stand for NaN (as 0 above)
+#pragma unroll
+      for (int d = 0; d < DT; ++d) o[d] = f32x16{} + __builtin_nanf("");
+    }
     if (id_next >= 0) {
       store_v(buf ^ 1, kb_next);
       ks[0] = x.ks[0];
