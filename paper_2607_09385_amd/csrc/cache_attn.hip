@@ -21,8 +21,8 @@
 // tokens of one channel in the same order.  V's scales differ from token to token, along the
 // sum, so they go into the weights: p_rj 2^e_jg is formed once per group of 32 channels (an
 // addition to the exponents: exact), and the codes alone are turned into bf16.  Weights are
-// rounded to bf16, the precision of the MFMA's operands (2^-9 of each weight on average, 2^-8
-// at most); l adds them before that rounding.
+// rounded to bf16, the precision of the MFMA's operands (off by 2^-8 of each weight at most, in
+// either direction); l adds them before that rounding.
 //
 // A page id outside the pool is a page without visible keys; keys behind the
 // sequence's length are never visible, whatever their bytes.
