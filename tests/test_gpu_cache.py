@@ -489,6 +489,28 @@ def test_tiles_of_unequal_lists(name, Hq, H, D, S, lens, kw):
     check_attention(name, pool, table, np.array(lens), bf16(rng, (len(lens), Hq, S, D)), D ** -0.5, **kw)
 
 
+@pytest.mark.parametrize("name,B,Hq,H,D,S,hi,zero,keep", [
+    ("ragged", 300, 4, 2, 64, 1, 1900, 0.3, None), ("few of many", 1000, 2, 1, 128, 2, 1700, 0.97, None),
+    ("one of many", 130, 4, 4, 64, 1, 1900, 1.0, None), ("masked", 40, 8, 4, 64, 1, 1900, 0.2, 0.3),
+    ("masked drafts", 70, 8, 2, 128, 5, 1800, 0.1, 0.1), ("none", 90, 4, 2, 64, 1, 1900, 2.0, None)])
+def test_many_sequences_and_empty_ones(name, B, Hq, H, D, S, hi, zero, keep):
+    """More sequences or lists than a wave has lanes, many of them without a page."""
+    rng = np.random.default_rng(B)
+    lens = rng.integers(1, hi, B)
+    lens[rng.random(B) < zero] = 0
+    if zero == 1.0:
+        lens[B - 1] = hi
+    pool = random_pool(rng, 150, H, D, 122, 129)
+    table = rng.integers(0, 150, (B, 30)).astype(np.int32)
+    kw = {} if keep is None else {"block_mask": (rng.random((B, H, 30)) < keep).astype(np.uint8)}
+    q = bf16(rng, (B, Hq, S, D))
+    if zero > 1.0:
+        out, lse = steel().attn_cache(gpu(q), gpu(pool), ints(table), ints(lens))
+        assert not out.any() and torch.isneginf(lse).all()
+    else:
+        check_attention(name, pool, table, lens, q, D ** -0.5, **kw)
+
+
 @pytest.mark.parametrize("S,D,keep", [(1, 128, 0.1), (2, 64, 0.3), (100, 128, 0.2)])
 def test_long_with_a_page_mask(S, D, keep):
     rng = np.random.default_rng(S)
