@@ -833,8 +833,8 @@ __global__ __launch_bounds__(64 * kWaves) void k_cache_join(CacheArgs a, SplitAr
 // registers until the present page is done.
 //
 // Bound by the MFMAs and the exponentials between them: 1000 queries of 32 heads against 12000
-// keys of 8 heads of 128 (188 GFLOP) 204 us with the join, 925 TFLOP/s; a large bf16 matrix
-// product reaches 1256 on the same card.  MFMAs take 38% of the cycles, VALU 43%, and the two
+// keys of 8 heads of 128 (188 GFLOP) 198 us with the join, 950 TFLOP/s; a large bf16 matrix
+// product reaches 1256 on the same card.  MFMAs take 40% of the cycles, VALU 44%, and the two
 // hardly overlap.  Two workgroups per CU; K Q^T costs twice its MFMA
 // time for the two parts of Q and is still no dearer than in bf16 (64 cycles for 64
 // channels, twice, against 4 x 33), without conversions or LDS traffic of bf16 keys.
