@@ -179,16 +179,19 @@ def fork(table, lens, refs, parent):
 def grow(table, lens, refs, new):
     """(table, lens, refs, src, dst, left)."""
     B, M = table.shape
-    t, l, r = np.array(table), np.array(lens), np.array(refs)
+    P = len(refs)
+    # pages behind the pool stand in for missing ones, to count them as if they were there
+    t, l, r = np.array(table), np.array(lens), np.concatenate((refs, np.zeros(B * (M + 1), np.int32)))
     src, dst = np.full(B, -1, np.int32), np.full(B, -1, np.int32)
     free = [p for p in range(len(r)) if r[p] == 0]
+    there = sum(p < P for p in free)
     used = 0
     narrow = False
 
     def take():
         nonlocal used
         used += 1
-        return free[used - 1] if used <= len(free) else None
+        return free[used - 1]
 
     for b in range(B):
         n, have = max(int(new[b]), 0), max(int(l[b]), 0)
@@ -196,25 +199,23 @@ def grow(table, lens, refs, new):
             narrow = True
             continue
         last = -(-have // PAGE) - 1
-        if n and have % PAGE and 0 <= t[b, last] < len(r) and r[t[b, last]] > 1:
+        if n and have % PAGE and 0 <= t[b, last] < P and r[t[b, last]] > 1:
             p = take()
-            if p is not None:
-                src[b], dst[b] = t[b, last], p
-                r[t[b, last]] -= 1
-                r[p] += 1
-                t[b, last] = p
+            src[b], dst[b] = t[b, last], p
+            r[t[b, last]] -= 1
+            r[p] += 1
+            t[b, last] = p
         for kb in range(last + 1, -(-(have + n) // PAGE)):
             p = take()
-            if p is not None:
-                t[b, kb] = p
-                r[p] += 1
+            t[b, kb] = p
+            r[p] += 1
         l[b] = have + n
-    left = len(free) - used
+    left = there - used
     if narrow or left < 0:
         none = np.full(B, -1, np.int32)
         return (np.array(table), np.array(lens), np.array(refs), none, none.copy(),
                 -2 ** 31 if narrow else left)
-    return t, l, r, src, dst, left
+    return t, l, r[:P], src, dst, left
 
 
 def compact(pages, table, lens, refs):
