@@ -384,7 +384,9 @@ int steel_attn_fwd_noalloc(const void* q, const void* k, const void* v,
  * A token whose position is negative, whose entry lies past the table or whose page does
  * not exist is dropped.  Two rows of one call that write the same slot (a shared
  * page written without steel_pages_grow and steel_pages_copy) leave either's
- * bytes in it.
+ * bytes in it.  lens has to count the new tokens: after a growth that did not fit it does
+ * not, and the positions would be those of tokens that are there; pass n_new then
+ * as steel_pages_grow_ex's took (0: nothing is written).
  */
 int steel_cache_append(const void* k, const void* v, long long k_sb, long long k_sh,
                        long long k_ss, long long v_sb, long long v_sh, long long v_ss,
@@ -472,6 +474,11 @@ int steel_pages_fork(const int32_t* page_table, const int32_t* lens, int32_t* re
  *   left       int32 [1]: free pages that remain.  Negative: that many were missing,
  *              or INT32_MIN: a row would need more than max_pages entries; then
  *              nothing has changed and every src and dst is -1
+ *   took       (steel_pages_grow_ex) int32 [B], or NULL: the tokens that there is room for,
+ *              max(n_new[b], 0), or 0 in every row where nothing has changed.  As n_new of
+ *              the calls that write and read the new tokens it makes a step that does
+ *              not fit one that does nothing, without a look at left from the host (as
+ *              in a graph).  It may not alias n_new
  *   workspace  at least steel_pages_workspace_bytes
  * n_pages up to 2^22.
  */
@@ -480,6 +487,11 @@ size_t steel_pages_workspace_bytes(int n_pages, int B);
 int steel_pages_grow(int32_t* page_table, int32_t* lens, int32_t* refs, const int32_t* n_new,
                      int32_t* src, int32_t* dst, int32_t* left, int B, int max_pages, int n_pages,
                      void* workspace, size_t workspace_bytes, void* stream);
+
+int steel_pages_grow_ex(int32_t* page_table, int32_t* lens, int32_t* refs, const int32_t* n_new,
+                        int32_t* src, int32_t* dst, int32_t* left, int32_t* took, int B,
+                        int max_pages, int n_pages, void* workspace, size_t workspace_bytes,
+                        void* stream);
 
 /*
  * Copies page src[i] onto page dst[i] for i < n, in each of ``layers`` pools

@@ -3,13 +3,18 @@
 ``pages`` is a uint8 pool [n_pages, Hkv, 68 * D] (include/steel.h has the layout: 64
 tokens a page, 4.25 bits a value), ``page_table`` int32 [B, max_pages] the pages of each
 sequence, ``lens`` int32 [B] their tokens and ``refs`` int32 [n_pages] how many rows
-hold each page (0: free).  A decoding step, its pool shared by all layers' tables:
+hold each page (0: free).  A decoding step, its table shared by all layers' pools:
 
-    src, dst, left = pages_grow(page_table, lens, refs, n_new)   # once a step
-    for pool in pools:                                           # every layer
+    src, dst, left = pages_grow(page_table, lens, refs, n_new, took=took)   # once a step
+    for pool in pools:                                                      # every layer
         pages_copy(pool, src, dst)                # pages that forked rows write into
-        cache_append(k, v, pool, page_table, lens, new=n_new)
-        out, lse = attn_cache(q, pool, page_table, lens, new=n_new)
+        cache_append(k, v, pool, page_table, lens, new=took)
+        out, lse = attn_cache(q, pool, page_table, lens, new=took)
+
+``took`` (int32 [B], like ``n_new``) is what there was room for: ``n_new``, or 0 everywhere
+where the pool is too full.  Such a step changes nothing and its ``out`` is 0; ``left`` is
+negative then, for the host to see when it looks next.  With ``n_new`` in the place of ``took``
+it would write over tokens that are there, so ``left`` has to be looked at first.
 
 Everything stays on the device: no call waits for the host, so a step may be captured
 into a graph.  Tensors that a call makes belong to the stream it runs on.
@@ -228,25 +233,29 @@ def pages_fork(page_table, lens, refs, parent, *, stream=None):
     return table, length
 
 
-def pages_grow(page_table, lens, refs, new, *, stream=None):
+def pages_grow(page_table, lens, refs, new, *, took=None, stream=None):
     """Room for new[b] (int32 [B]) more tokens of every sequence: page_table, lens and
     refs are updated, the lowest free pages taken first.  Returns (src, dst, left): the
     pages that ``pages_copy`` has to copy before the new tokens are written (int32
     [B], -1: none; rows that write into a page which other rows hold get their own) and
-    the free pages that remain (int32 [1]; negative: too few, nothing has changed)."""
+    the free pages that remain (int32 [1]; negative: too few, nothing has changed).
+
+    took: int32 [B] that is filled with the tokens each sequence got room for, max(new[b], 0)
+    or 0 where nothing has changed: what the calls that follow take as their ``new``."""
     _gpu("page_table", page_table)
     device = page_table.device
     B, M, tp, lp = _table(page_table, lens, device)
     n_pages = _numel("refs", refs)
     rp = _ints("refs", refs, (n_pages,), device)
     np_ = _ints("new", new, (B,), device)
+    kp = None if took is None else _ints("took", took, (B,), device)
     nbytes = _bytes("steel_pages_workspace_bytes", n_pages, B)
     i32 = page_table.dtype
     n = nbytes // 4
     made, = _empty(stream, page_table, ((n + 2 * B + 1,), i32))
     ws, src, dst, left = made.split_with_sizes((n, B, B, 1))
-    _call(_lib.load().steel_pages_grow, device, stream, tp, lp, rp, np_, src.data_ptr(),
-          dst.data_ptr(), left.data_ptr(), B, M, n_pages, ws.data_ptr(), nbytes)
+    _call(_lib.load().steel_pages_grow_ex, device, stream, tp, lp, rp, np_, src.data_ptr(),
+          dst.data_ptr(), left.data_ptr(), kp, B, M, n_pages, ws.data_ptr(), nbytes)
     return src, dst, left
 
 

@@ -79,10 +79,10 @@ hipError_t launch_pages_fork(const int32_t* table, const int32_t* lens, int32_t*
                              int B_out, int M, int n_pages, hipStream_t s);
 
 // Workspace of pages_grow: {writers, last writer} per page, the free pages by
-// rank, the first rank of each sequence.
+// rank, the first rank of each sequence.  took: may be nullptr.
 hipError_t launch_pages_grow(int32_t* table, int32_t* lens, int32_t* refs, const int32_t* fresh,
-                             int32_t* src, int32_t* dst, int32_t* left, int B, int M, int n_pages,
-                             int32_t* ws, hipStream_t s);
+                             int32_t* src, int32_t* dst, int32_t* left, int32_t* took, int B, int M,
+                             int n_pages, int32_t* ws, hipStream_t s);
 
 hipError_t launch_pages_copy(uint8_t* pages, long long layer_bytes, long long page_bytes, int layers,
                              const int32_t* src, const int32_t* dst, int n, int n_pages, hipStream_t s);

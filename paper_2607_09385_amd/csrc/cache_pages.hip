@@ -117,7 +117,8 @@ __global__ __launch_bounds__(1024) void k_pages_grow(int32_t* __restrict__ table
                                                      const int32_t* __restrict__ fresh,
                                                      int32_t* __restrict__ src,
                                                      int32_t* __restrict__ dst,
-                                                     int32_t* __restrict__ left, int B, int M,
+                                                     int32_t* __restrict__ left,
+                                                     int32_t* __restrict__ took, int B, int M,
                                                      int n_pages, int32_t* ws) {
   constexpr int T = 1024;
   int32_t* writers = ws;
@@ -193,7 +194,10 @@ __global__ __launch_bounds__(1024) void k_pages_grow(int32_t* __restrict__ table
   const bool fits = !narrow && total >= demand;
   if (tid == 0) left[0] = narrow ? INT_MIN : total - demand;
   if (!fits) {
-    for (int b = tid; b < B; b += T) src[b] = -1;
+    for (int b = tid; b < B; b += T) {
+      src[b] = -1;
+      if (took != nullptr) took[b] = 0;
+    }
     return;
   }
   // the first `demand` of them in order
@@ -228,7 +232,11 @@ __global__ __launch_bounds__(1024) void k_pages_grow(int32_t* __restrict__ table
     }
   }
   __syncthreads();
-  for (int b = tid; b < B; b += T) lens[b] = max(lens[b], 0) + max(fresh[b], 0);
+  for (int b = tid; b < B; b += T) {
+    const int more = max(fresh[b], 0);
+    lens[b] = max(lens[b], 0) + more;
+    if (took != nullptr) took[b] = more;
+  }
 }
 
 // The same for up to 1024 sequences and 2^16 pages, with one sequence per thread: what a
@@ -241,7 +249,8 @@ __global__ __launch_bounds__(1024) void k_pages_grow_few(int32_t* __restrict__ t
                                                          const int32_t* __restrict__ fresh,
                                                          int32_t* __restrict__ src,
                                                          int32_t* __restrict__ dst,
-                                                         int32_t* __restrict__ left, int B, int M,
+                                                         int32_t* __restrict__ left,
+                                                         int32_t* __restrict__ took, int B, int M,
                                                          int n_pages) {
   constexpr int T = 1024;
   __shared__ unsigned long long free_set[T];  // bit i of word w: page 64 w + i is free
@@ -295,6 +304,7 @@ __global__ __launch_bounds__(1024) void k_pages_grow_few(int32_t* __restrict__ t
   if (tid < B) {
     src[tid] = fits && copy ? id : -1;
     if (!(fits && copy)) dst[tid] = -1;
+    if (took != nullptr) took[tid] = fits ? more : 0;
     if (fits) lens[tid] = (int)to;
     if (fits && copy) atomicAdd(refs + id, -1);
   }
@@ -312,14 +322,14 @@ __global__ __launch_bounds__(1024) void k_pages_grow_few(int32_t* __restrict__ t
 }
 
 hipError_t launch_pages_grow(int32_t* table, int32_t* lens, int32_t* refs, const int32_t* fresh,
-                             int32_t* src, int32_t* dst, int32_t* left, int B, int M, int n_pages,
-                             int32_t* ws, hipStream_t s) {
+                             int32_t* src, int32_t* dst, int32_t* left, int32_t* took, int B, int M,
+                             int n_pages, int32_t* ws, hipStream_t s) {
   if (B <= 1024 && n_pages <= 65536)
     hipLaunchKernelGGL(k_pages_grow_few, dim3(1), dim3(1024), 0, s, table, lens, refs, fresh, src, dst,
-                       left, B, M, n_pages);
+                       left, took, B, M, n_pages);
   else
     hipLaunchKernelGGL(k_pages_grow, dim3(1), dim3(1024), 0, s, table, lens, refs, fresh, src, dst,
-                       left, B, M, n_pages, ws);
+                       left, took, B, M, n_pages, ws);
   return hipGetLastError();
 }
 

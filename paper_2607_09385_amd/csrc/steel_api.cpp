@@ -762,17 +762,28 @@ size_t steel_pages_workspace_bytes(int n_pages, int B) {
 int steel_pages_grow(int32_t* page_table, int32_t* lens, int32_t* refs, const int32_t* n_new,
                      int32_t* src, int32_t* dst, int32_t* left, int B, int max_pages, int n_pages,
                      void* workspace, size_t workspace_bytes, void* stream) {
+  return steel_pages_grow_ex(page_table, lens, refs, n_new, src, dst, left, nullptr, B, max_pages,
+                             n_pages, workspace, workspace_bytes, stream);
+}
+
+int steel_pages_grow_ex(int32_t* page_table, int32_t* lens, int32_t* refs, const int32_t* n_new,
+                        int32_t* src, int32_t* dst, int32_t* left, int32_t* took, int B,
+                        int max_pages, int n_pages, void* workspace, size_t workspace_bytes,
+                        void* stream) {
   g_err.clear();
   if (!page_table || !lens || !refs || !n_new || !src || !dst || !left)
     return fail(STEEL_ERR_INVALID_ARGUMENT,
                 "page_table, lens, refs, n_new, src, dst and left must be non-NULL");
+  if (took == n_new)
+    return fail(STEEL_ERR_INVALID_ARGUMENT, "took may not alias n_new");
   int rc = check_pages(B, max_pages, n_pages);
   if (rc != STEEL_OK) return rc;
   if ((rc = check_bytes(workspace, workspace_bytes,
                         sizeof(int32_t) * steel::pages_ws_ints(n_pages, B))) != STEEL_OK)
     return rc;
-  const hipError_t e = steel::launch_pages_grow(page_table, lens, refs, n_new, src, dst, left, B,
-                                                max_pages, n_pages, static_cast<int32_t*>(workspace),
+  const hipError_t e = steel::launch_pages_grow(page_table, lens, refs, n_new, src, dst, left, took,
+                                                B, max_pages, n_pages,
+                                                static_cast<int32_t*>(workspace),
                                                 static_cast<hipStream_t>(stream));
   return e == hipSuccess ? STEEL_OK : hip_fail(e, "launching the growth");
 }

@@ -1,0 +1,16 @@
+"""Refusals of the page calls' longer forms (no GPU needed: every check runs before any HIP
+call)."""
+from paper_2607_09385_amd import _lib
+
+F, G = 0x100000, 0x101000  # aligned, never dereferenced on the checked paths
+
+
+def test_growth_refuses_a_took_that_is_its_input():
+    lib = _lib.load()
+    n = lib.steel_pages_workspace_bytes(8, 2)
+    assert lib.steel_pages_grow_ex(F, F, F, G, F, F, F, G, 2, 4, 8, F, n, None) == 1
+    assert "alias" in _lib.last_error()
+    assert lib.steel_pages_grow_ex(F, F, F, G, F, F, None, F, 2, 4, 8, F, n, None) == 1
+    assert lib.steel_pages_grow_ex(F, F, F, G, F, F, F, F, 2, 4, 8, F, n - 256, None) == 1
+    assert "smaller" in _lib.last_error()
+    assert lib.steel_pages_grow_ex(F, F, F, G, F, F, F, F, 0, 4, 8, F, n, None) == 1
