@@ -465,8 +465,9 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(D, NT)) void k_cache_to
       const int zb = listed ? z / a.Hkv : z, zg = listed ? z % a.Hkv : 0;
       const Span sp = make_span(a, zb, 0, rows);
       const float zero[4] = {0.f, 0.f, 0.f, 0.f};
-      for (int i = threadIdx.x; i < heads * rows * (D / 4); i += 64 * kWaves)
-        store_row<4>(a, sp, D, zb, zg + i / (D / 4) / rows, i / (D / 4) % rows, i % (D / 4) * 4, zero, 0.f, 0.f);
+      constexpr int C = D / 4;  // threads of a row; heads * rows alone is below 2^31
+      for (int i = threadIdx.x / C; i < heads * rows; i += 64 * kWaves / C)
+        store_row<4>(a, sp, D, zb, zg + i / rows, i % rows, threadIdx.x % C * 4, zero, 0.f, 0.f);
     }
   }
 
