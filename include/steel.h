@@ -507,12 +507,21 @@ int steel_pages_copy(uint8_t* pages, const int32_t* src, const int32_t* dst, int
  * Moves the live pages (refs > 0) to the front of the pool, in each of ``layers``
  * pools: with n of them, those numbered n or more move, in order, to the free
  * pages below n, in order.  page_table (the held entries) and refs follow.
+ * Live pages that no row of this table holds (a kept prefix, another table) move too.
  *   live       int32 [1]: n
+ *   to         (steel_pages_compact_ex) int32 [n_pages], or NULL: the number that each live
+ *              page has now, by the one it had, and -1 for free ones: what other holders
+ *              look theirs up in.  It may not alias refs
  *   workspace  at least steel_pages_workspace_bytes
  */
 int steel_pages_compact(uint8_t* pages, int32_t* page_table, const int32_t* lens, int32_t* refs,
                         int32_t* live, int B, int max_pages, int layers, int n_pages,
                         size_t page_bytes, void* workspace, size_t workspace_bytes, void* stream);
+
+int steel_pages_compact_ex(uint8_t* pages, int32_t* page_table, const int32_t* lens, int32_t* refs,
+                           int32_t* live, int32_t* to, int B, int max_pages, int layers,
+                           int n_pages, size_t page_bytes, void* workspace, size_t workspace_bytes,
+                           void* stream);
 
 /* Text of the last non-OK status returned on the calling thread ("" if none). */
 const char* steel_last_error(void);

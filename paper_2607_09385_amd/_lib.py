@@ -103,6 +103,9 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.steel_pages_compact.restype = c_int
     lib.steel_pages_compact.argtypes = [c_void_p] * 5 + [c_int] * 4 + [c_size_t, c_void_p, c_size_t,
                                                                        c_void_p]
+    lib.steel_pages_compact_ex.restype = c_int
+    lib.steel_pages_compact_ex.argtypes = [c_void_p] * 6 + [c_int] * 4 + [c_size_t, c_void_p, c_size_t,
+                                                                          c_void_p]
     lib.steel_last_error.restype = ctypes.c_char_p
     lib.steel_last_error.argtypes = []
     lib.steel_version.restype = ctypes.c_char_p

@@ -269,17 +269,22 @@ def pages_copy(pages, src, dst, *, stream=None):
           _ints("src", src, (n,), device), _ints("dst", dst, (n,), device), n, layers, n_pages, nbytes)
 
 
-def pages_compact(pages, page_table, lens, refs, *, stream=None):
+def pages_compact(pages, page_table, lens, refs, *, to=None, stream=None):
     """Move the live pages (refs > 0) of a pool, or of every layer of a [layers, ...]
-    pool, to its front; page_table and refs follow.  Returns their number (int32 [1])."""
+    pool, to its front; page_table and refs follow.  Returns their number (int32 [1]).
+
+    to: int32 [n_pages] that is filled with the number each live page has now, by the one it
+    had (-1: free).  Pages that no row of ``page_table`` holds (a kept prefix, another table)
+    move too, and this is where their holders find them."""
     layers, n_pages, page_bytes = _layers(pages)
     device = pages.device
     B, M, tp, lp = _table(page_table, lens, device)
     rp = _ints("refs", refs, (n_pages,), device)
+    op = None if to is None else _ints("to", to, (n_pages,), device)
     nbytes = _bytes("steel_pages_workspace_bytes", n_pages, B)
     i32 = page_table.dtype
     made, = _empty(stream, pages, ((nbytes // 4 + 1,), i32))
     ws, live = made.split_with_sizes((nbytes // 4, 1))
-    _call(_lib.load().steel_pages_compact, device, stream, pages.data_ptr(), tp, lp, rp,
-          live.data_ptr(), B, M, layers, n_pages, page_bytes, ws.data_ptr(), nbytes)
+    _call(_lib.load().steel_pages_compact_ex, device, stream, pages.data_ptr(), tp, lp, rp,
+          live.data_ptr(), op, B, M, layers, n_pages, page_bytes, ws.data_ptr(), nbytes)
     return live

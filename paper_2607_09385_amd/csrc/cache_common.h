@@ -88,10 +88,11 @@ hipError_t launch_pages_copy(uint8_t* pages, long long layer_bytes, long long pa
                              const int32_t* src, const int32_t* dst, int n, int n_pages, hipStream_t s);
 
 // Workspace of pages_compact: live pages per chunk, {live, moves}, holes and
-// moved pages by rank, the rank of each moved page.
+// moved pages by rank, the rank of each moved page.  to: may be nullptr.
 hipError_t launch_pages_compact(uint8_t* pages, long long layer_bytes, long long page_bytes,
                                 int layers, int32_t* table, const int32_t* lens, int32_t* refs,
-                                int32_t* live, int B, int M, int n_pages, int32_t* ws, hipStream_t s);
+                                int32_t* live, int32_t* to, int B, int M, int n_pages, int32_t* ws,
+                                hipStream_t s);
 
 inline size_t pages_ws_ints(int n_pages, int B) {
   return 3 * (size_t)n_pages + (size_t)B + kMaxPages / kPageChunk + 64;

@@ -388,13 +388,15 @@ __global__ __launch_bounds__(256) void k_pages_count(const int32_t* __restrict__
   if (threadIdx.x == 0) chunk_live[blockIdx.x] = all;
 }
 
-// head: {live, moves}; hole[r], mover[r]: the r-th move; rank[p]: the move of page p
+// head: {live, moves}; hole[r], mover[r]: the r-th move; rank[p]: the move of page p; to[p] (may
+// be nullptr): p, or -1 for a free page (k_pages_move changes those that move)
 __global__ __launch_bounds__(256) void k_pages_rank(const int32_t* __restrict__ refs, int n_pages,
                                                     const int32_t* __restrict__ chunk_live,
                                                     int32_t* __restrict__ head,
                                                     int32_t* __restrict__ hole,
                                                     int32_t* __restrict__ mover,
                                                     int32_t* __restrict__ rank,
+                                                    int32_t* __restrict__ to,
                                                     int32_t* __restrict__ live_out) {
   constexpr int U = kPageChunk / 256;
   __shared__ int sums[4];
@@ -428,6 +430,7 @@ __global__ __launch_bounds__(256) void k_pages_rank(const int32_t* __restrict__ 
   for (int u = 0; u < U; ++u) {
     const int p = p0 + u;
     const bool l = (f >> u) & 1;
+    if (to != nullptr && p < n_pages) to[p] = l ? p : -1;
     if (l && p >= live) {
       mover[before - stay] = p;
       rank[p] = before - stay;
@@ -450,6 +453,7 @@ __global__ __launch_bounds__(1024) void k_pages_rank_few(const int32_t* __restri
                                                          int32_t* __restrict__ hole,
                                                          int32_t* __restrict__ mover,
                                                          int32_t* __restrict__ rank,
+                                                         int32_t* __restrict__ to,
                                                          int32_t* __restrict__ live_out) {
   constexpr int T = 1024;
   __shared__ unsigned long long live_set[T];
@@ -458,7 +462,9 @@ __global__ __launch_bounds__(1024) void k_pages_rank_few(const int32_t* __restri
   const int tid = threadIdx.x;
   for (int p0 = 0; p0 < n_pages; p0 += T) {
     const int p = p0 + tid;
-    const unsigned long long f = __ballot(p < n_pages && refs[p < n_pages ? p : 0] > 0);
+    const bool l = p < n_pages && refs[p < n_pages ? p : 0] > 0;
+    if (to != nullptr && p < n_pages) to[p] = l ? p : -1;
+    const unsigned long long f = __ballot(l);
     if ((tid & 63) == 0) live_set[p0 / 64 + (tid >> 6)] = f;
   }
   if (tid == 0) kept = 0;
@@ -508,7 +514,8 @@ __global__ __launch_bounds__(256) void k_pages_move(uint8_t* pages, long long la
                                                     int n_pages, const int32_t* __restrict__ head,
                                                     const int32_t* __restrict__ hole,
                                                     const int32_t* __restrict__ mover,
-                                                    const int32_t* __restrict__ rank) {
+                                                    const int32_t* __restrict__ rank,
+                                                    int32_t* __restrict__ to) {
   const int live = head[0], moves = head[1];
   if ((int)blockIdx.x < rows) {
     const int b = blockIdx.x, n = held_pages(lens[b], M);
@@ -522,6 +529,7 @@ __global__ __launch_bounds__(256) void k_pages_move(uint8_t* pages, long long la
       for (int r = threadIdx.x; r < moves; r += 256) {
         refs[hole[r]] = refs[mover[r]];
         refs[mover[r]] = 0;
+        if (to != nullptr) to[mover[r]] = hole[r];
       }
     return;
   }
@@ -535,7 +543,8 @@ __global__ __launch_bounds__(256) void k_pages_move(uint8_t* pages, long long la
 
 hipError_t launch_pages_compact(uint8_t* pages, long long layer_bytes, long long page_bytes,
                                 int layers, int32_t* table, const int32_t* lens, int32_t* refs,
-                                int32_t* live, int B, int M, int n_pages, int32_t* ws, hipStream_t s) {
+                                int32_t* live, int32_t* to, int B, int M, int n_pages, int32_t* ws,
+                                hipStream_t s) {
   const int chunks = (n_pages + kPageChunk - 1) / kPageChunk;
   int32_t* hole = ws;
   int32_t* mover = hole + n_pages;
@@ -547,14 +556,14 @@ hipError_t launch_pages_compact(uint8_t* pages, long long layer_bytes, long long
   const int copiers = (int)(most < 2048 ? (most > 0 ? most : 1) : 2048);
   if (n_pages <= 65536) {
     hipLaunchKernelGGL(k_pages_rank_few, dim3(1), dim3(1024), 0, s, refs, n_pages, head, hole, mover,
-                       rank, live);
+                       rank, to, live);
   } else {
     hipLaunchKernelGGL(k_pages_count, dim3(chunks), dim3(256), 0, s, refs, n_pages, chunk_live);
     hipLaunchKernelGGL(k_pages_rank, dim3(chunks), dim3(256), 0, s, refs, n_pages, chunk_live, head,
-                       hole, mover, rank, live);
+                       hole, mover, rank, to, live);
   }
   hipLaunchKernelGGL(k_pages_move, dim3(B + copiers), dim3(256), 0, s, pages, layer_bytes, page_bytes,
-                     layers, pieces, table, lens, refs, B, M, n_pages, head, hole, mover, rank);
+                     layers, pieces, table, lens, refs, B, M, n_pages, head, hole, mover, rank, to);
   return hipGetLastError();
 }
 

@@ -807,9 +807,18 @@ int steel_pages_copy(uint8_t* pages, const int32_t* src, const int32_t* dst, int
 int steel_pages_compact(uint8_t* pages, int32_t* page_table, const int32_t* lens, int32_t* refs,
                         int32_t* live, int B, int max_pages, int layers, int n_pages,
                         size_t page_bytes, void* workspace, size_t workspace_bytes, void* stream) {
+  return steel_pages_compact_ex(pages, page_table, lens, refs, live, nullptr, B, max_pages, layers,
+                                n_pages, page_bytes, workspace, workspace_bytes, stream);
+}
+
+int steel_pages_compact_ex(uint8_t* pages, int32_t* page_table, const int32_t* lens, int32_t* refs,
+                           int32_t* live, int32_t* to, int B, int max_pages, int layers,
+                           int n_pages, size_t page_bytes, void* workspace, size_t workspace_bytes,
+                           void* stream) {
   g_err.clear();
   if (!page_table || !lens || !refs || !live)
     return fail(STEEL_ERR_INVALID_ARGUMENT, "page_table, lens, refs and live must be non-NULL");
+  if (to == refs) return fail(STEEL_ERR_INVALID_ARGUMENT, "to may not alias refs");
   int rc = check_pool(pages, layers, n_pages, page_bytes);
   if (rc == STEEL_OK) rc = check_pages(B, max_pages, n_pages);
   if (rc != STEEL_OK) return rc;
@@ -818,7 +827,7 @@ int steel_pages_compact(uint8_t* pages, int32_t* page_table, const int32_t* lens
     return rc;
   const hipError_t e = steel::launch_pages_compact(
       pages, (long long)(page_bytes * (size_t)n_pages), (long long)page_bytes, layers, page_table,
-      lens, refs, live, B, max_pages, n_pages, static_cast<int32_t*>(workspace),
+      lens, refs, live, to, B, max_pages, n_pages, static_cast<int32_t*>(workspace),
       static_cast<hipStream_t>(stream));
   return e == hipSuccess ? STEEL_OK : hip_fail(e, "launching the compaction");
 }

@@ -14,3 +14,12 @@ def test_growth_refuses_a_took_that_is_its_input():
     assert lib.steel_pages_grow_ex(F, F, F, G, F, F, F, F, 2, 4, 8, F, n - 256, None) == 1
     assert "smaller" in _lib.last_error()
     assert lib.steel_pages_grow_ex(F, F, F, G, F, F, F, F, 0, 4, 8, F, n, None) == 1
+
+
+def test_compaction_refuses_a_map_over_its_counts():
+    lib = _lib.load()
+    n = lib.steel_pages_workspace_bytes(8, 2)
+    assert lib.steel_pages_compact_ex(F, F, F, G, F, G, 2, 4, 1, 8, 64, F, n, None) == 1
+    assert "alias" in _lib.last_error()
+    assert lib.steel_pages_compact_ex(F, F, F, G, None, F, 2, 4, 1, 8, 64, F, n, None) == 1
+    assert lib.steel_pages_compact_ex(F, F, F, G, F, F, 2, 4, 1, 8, 64, F, n - 256, None) == 1
