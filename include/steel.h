@@ -479,10 +479,12 @@ int steel_pages_fork(const int32_t* page_table, const int32_t* lens, int32_t* re
  *              the calls that write and read the new tokens it makes a step that does
  *              not fit one that does nothing, without a look at left from the host (as
  *              in a graph).  It may not alias n_new
- *   workspace  at least steel_pages_workspace_bytes
+ *   workspace  at least steel_pages_workspace_bytes, or NULL where
+ *              steel_pages_grow_workspace_bytes is 256: none is used
  * n_pages up to 2^22.
  */
 size_t steel_pages_workspace_bytes(int n_pages, int B);
+size_t steel_pages_grow_workspace_bytes(int n_pages, int B);
 
 int steel_pages_grow(int32_t* page_table, int32_t* lens, int32_t* refs, const int32_t* n_new,
                      int32_t* src, int32_t* dst, int32_t* left, int B, int max_pages, int n_pages,

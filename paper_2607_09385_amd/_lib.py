@@ -94,6 +94,8 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.steel_pages_fork.argtypes = [c_void_p] * 6 + [c_int] * 4 + [c_void_p]
     lib.steel_pages_workspace_bytes.restype = c_size_t
     lib.steel_pages_workspace_bytes.argtypes = [c_int] * 2
+    lib.steel_pages_grow_workspace_bytes.restype = c_size_t
+    lib.steel_pages_grow_workspace_bytes.argtypes = [c_int] * 2
     lib.steel_pages_grow.restype = c_int
     lib.steel_pages_grow.argtypes = [c_void_p] * 7 + [c_int] * 3 + [c_void_p, c_size_t, c_void_p]
     lib.steel_pages_grow_ex.restype = c_int

@@ -249,13 +249,15 @@ def pages_grow(page_table, lens, refs, new, *, took=None, stream=None):
     rp = _ints("refs", refs, (n_pages,), device)
     np_ = _ints("new", new, (B,), device)
     kp = None if took is None else _ints("took", took, (B,), device)
-    nbytes = _bytes("steel_pages_workspace_bytes", n_pages, B)
-    i32 = page_table.dtype
-    n = nbytes // 4
-    made, = _empty(stream, page_table, ((n + 2 * B + 1,), i32))
-    ws, src, dst, left = made.split_with_sizes((n, B, B, 1))
+    nbytes = _bytes("steel_pages_grow_workspace_bytes", n_pages, B)
+    ws = None  # 256 bytes: none is used
+    if nbytes > 256:
+        ws, = _empty(stream, page_table, ((nbytes,), _torch().uint8))
+    made, = _empty(stream, page_table, ((2 * B + 1,), page_table.dtype))
+    src, dst, left = made.split_with_sizes((B, B, 1))
     _call(_lib.load().steel_pages_grow_ex, device, stream, tp, lp, rp, np_, src.data_ptr(),
-          dst.data_ptr(), left.data_ptr(), kp, B, M, n_pages, ws.data_ptr(), nbytes)
+          dst.data_ptr(), left.data_ptr(), kp, B, M, n_pages,
+          None if ws is None else ws.data_ptr(), nbytes)
     return src, dst, left
 
 
@@ -282,9 +284,7 @@ def pages_compact(pages, page_table, lens, refs, *, to=None, stream=None):
     rp = _ints("refs", refs, (n_pages,), device)
     op = None if to is None else _ints("to", to, (n_pages,), device)
     nbytes = _bytes("steel_pages_workspace_bytes", n_pages, B)
-    i32 = page_table.dtype
-    made, = _empty(stream, pages, ((nbytes // 4 + 1,), i32))
-    ws, live = made.split_with_sizes((nbytes // 4, 1))
+    ws, live = _empty(stream, pages, ((nbytes,), _torch().uint8), ((1,), page_table.dtype))
     _call(_lib.load().steel_pages_compact_ex, device, stream, pages.data_ptr(), tp, lp, rp,
           live.data_ptr(), op, B, M, layers, n_pages, page_bytes, ws.data_ptr(), nbytes)
     return live

@@ -78,8 +78,11 @@ hipError_t launch_pages_fork(const int32_t* table, const int32_t* lens, int32_t*
                              const int32_t* parent, int32_t* table_out, int32_t* lens_out, int B_in,
                              int B_out, int M, int n_pages, hipStream_t s);
 
+// Up to 1024 rows and 2^16 pages one thread takes a row and LDS holds all that a growth needs.
+inline bool pages_few(int n_pages, int B) { return B <= 1024 && n_pages <= 65536; }
+
 // Workspace of pages_grow: {writers, last writer} per page, the free pages by
-// rank, the first rank of each sequence.  took: may be nullptr.
+// rank, the first rank of each sequence; none where pages_few.  took: may be nullptr.
 hipError_t launch_pages_grow(int32_t* table, int32_t* lens, int32_t* refs, const int32_t* fresh,
                              int32_t* src, int32_t* dst, int32_t* left, int32_t* took, int B, int M,
                              int n_pages, int32_t* ws, hipStream_t s);

@@ -324,7 +324,7 @@ __global__ __launch_bounds__(1024) void k_pages_grow_few(int32_t* __restrict__ t
 hipError_t launch_pages_grow(int32_t* table, int32_t* lens, int32_t* refs, const int32_t* fresh,
                              int32_t* src, int32_t* dst, int32_t* left, int32_t* took, int B, int M,
                              int n_pages, int32_t* ws, hipStream_t s) {
-  if (B <= 1024 && n_pages <= 65536)
+  if (pages_few(n_pages, B))
     hipLaunchKernelGGL(k_pages_grow_few, dim3(1), dim3(1024), 0, s, table, lens, refs, fresh, src, dst,
                        left, took, B, M, n_pages);
   else

@@ -759,6 +759,11 @@ size_t steel_pages_workspace_bytes(int n_pages, int B) {
   return align256(sizeof(int32_t) * steel::pages_ws_ints(n_pages, B));
 }
 
+size_t steel_pages_grow_workspace_bytes(int n_pages, int B) {
+  const size_t need = steel_pages_workspace_bytes(n_pages, B);
+  return need > 0 && steel::pages_few(n_pages, B) ? 256 : need;
+}
+
 int steel_pages_grow(int32_t* page_table, int32_t* lens, int32_t* refs, const int32_t* n_new,
                      int32_t* src, int32_t* dst, int32_t* left, int B, int max_pages, int n_pages,
                      void* workspace, size_t workspace_bytes, void* stream) {
@@ -778,7 +783,8 @@ int steel_pages_grow_ex(int32_t* page_table, int32_t* lens, int32_t* refs, const
     return fail(STEEL_ERR_INVALID_ARGUMENT, "took may not alias n_new");
   int rc = check_pages(B, max_pages, n_pages);
   if (rc != STEEL_OK) return rc;
-  if ((rc = check_bytes(workspace, workspace_bytes,
+  if (!(workspace == nullptr && steel::pages_few(n_pages, B)) &&
+      (rc = check_bytes(workspace, workspace_bytes,
                         sizeof(int32_t) * steel::pages_ws_ints(n_pages, B))) != STEEL_OK)
     return rc;
   const hipError_t e = steel::launch_pages_grow(page_table, lens, refs, n_new, src, dst, left, took,

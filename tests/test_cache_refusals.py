@@ -23,3 +23,15 @@ def test_compaction_refuses_a_map_over_its_counts():
     assert "alias" in _lib.last_error()
     assert lib.steel_pages_compact_ex(F, F, F, G, None, F, 2, 4, 1, 8, 64, F, n, None) == 1
     assert lib.steel_pages_compact_ex(F, F, F, G, F, F, 2, 4, 1, 8, 64, F, n - 256, None) == 1
+
+
+def test_growth_without_a_workspace():
+    """Only where none is used: up to 1024 rows and 65,536 pages."""
+    lib = _lib.load()
+    need = lib.steel_pages_grow_workspace_bytes
+    assert need(8, 2) == need(65536, 1024) == 256
+    for sizes in ((65537, 1), (8, 1025)):
+        assert need(*sizes) == lib.steel_pages_workspace_bytes(*sizes) > 256
+        assert lib.steel_pages_grow_ex(F, F, F, G, F, F, F, None, sizes[1], 4, sizes[0], None, 1 << 40, None) == 1
+        assert "workspace" in _lib.last_error()
+    assert need(0, 2) == 0 and need(8, 0) == 0
