@@ -436,9 +436,13 @@ int steel_cache_load(const uint8_t* pages, const int32_t* page_table, const int3
  * Results are bitwise reproducible run to run.
  *
  *   workspace   at least steel_attn_cache_workspace_bytes of the same sizes (0 after an
- *               argument error); where that is 256 none is used and it may be NULL
+ *               argument error); where that is 256 none is used and it may be NULL.
+ *               Without a block_mask steel_attn_cache_workspace_bytes_ex with masked = 0
+ *               will do: 8 B Hkv max_pages bytes less, the room for lists of live pages
  */
 size_t steel_attn_cache_workspace_bytes(int B, int Hq, int Hkv, int S_q, int D, int max_pages);
+size_t steel_attn_cache_workspace_bytes_ex(int B, int Hq, int Hkv, int S_q, int D, int max_pages,
+                                           int masked);
 
 int steel_attn_cache(const void* q, long long q_sb, long long q_sh, long long q_ss,
                      const uint8_t* pages, const int32_t* page_table, const int32_t* lens,

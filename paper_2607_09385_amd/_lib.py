@@ -87,6 +87,8 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.steel_cache_load.argtypes = [c_void_p] * 6 + [c_int] * 6 + [c_void_p]
     lib.steel_attn_cache_workspace_bytes.restype = c_size_t
     lib.steel_attn_cache_workspace_bytes.argtypes = [c_int] * 6
+    lib.steel_attn_cache_workspace_bytes_ex.restype = c_size_t
+    lib.steel_attn_cache_workspace_bytes_ex.argtypes = [c_int] * 7
     lib.steel_attn_cache.restype = c_int
     lib.steel_attn_cache.argtypes = [c_void_p] + [c_ll] * 3 + [c_void_p] * 7 + [c_int] * 7 \
         + [c_float] + [c_int] * 4 + [c_void_p, c_size_t, c_void_p]

@@ -204,7 +204,7 @@ def attn_cache(q, pages, page_table, lens, *, new=None, block_mask=None, window_
     elif lse.dtype != torch.float32 or lse.shape != rows or not lse.is_contiguous() \
             or lse.device != device:
         raise ValueError(f"lse must be a contiguous float32 tensor [B, Hq, S_q] on {device}")
-    nbytes = _bytes("steel_attn_cache_workspace_bytes", B, Hq, Hkv, S_q, D, M)
+    nbytes = _bytes("steel_attn_cache_workspace_bytes_ex", B, Hq, Hkv, S_q, D, M, mp is not None)
     ws = None  # 256 bytes: none is used
     if nbytes > 256:
         ws, = _empty(stream, pages, ((nbytes,), torch.uint8))

@@ -1237,7 +1237,7 @@ struct TokenPlan {
 // no second launch.  One token at 4 / 16 / 24 / 32 pages, whole against split: 8 heads of 128
 // 6.8 / 10.9 / 13.6 / 16.4 us against 11.3 / 13.7 / 13.7 / 13.7, 64 sequences of 8 heads
 // 10.4 / 19.5 / 27.2 / 32.9 us against 15.6 / 30.1 / 37.9 / 43.2.
-TokenPlan token_plan(int B, int Hkv, int rows, int D, int M, int pages) {
+TokenPlan token_plan(int B, int Hkv, int rows, int D, int M, int pages, bool masked) {
   TokenPlan p{};
   const long long lists = (long long)B * Hkv;
   const long long want = (lists * pages + 3) / 4;
@@ -1251,7 +1251,7 @@ TokenPlan token_plan(int B, int Hkv, int rows, int D, int M, int pages) {
   p.where = p.part + up(slots * D * sizeof(float));
   p.list = p.where + up((size_t)lists * sizeof(int2));
   p.counts = p.list + up((size_t)lists * M * sizeof(int2));
-  p.total = p.split ? p.counts + (size_t)lists * sizeof(int) : 0;
+  p.total = !p.split ? 0 : masked ? p.counts + (size_t)lists * sizeof(int) : p.list;
   return p;
 }
 
@@ -1282,9 +1282,10 @@ void launch_token(const CacheArgs& a, const TokenPlan& p, char* ws, int rows, hi
 // third tile of accumulators, which do not fit into registers beside two.
 constexpr int kTokenRows = 32;
 
-size_t cache_attn_ws(int B, int Hq, int Hkv, int S_q, int D, int M) {
+size_t cache_attn_ws(int B, int Hq, int Hkv, int S_q, int D, int M, bool masked) {
   const int rows = S_q * (Hq / Hkv);
-  return rows <= kTokenRows ? token_plan(B, Hkv, rows, D, M, M).total : chunk_plan(B, Hkv, rows, D, M).total;
+  return rows <= kTokenRows ? token_plan(B, Hkv, rows, D, M, M, masked).total
+                            : chunk_plan(B, Hkv, rows, D, M).total;
 }
 
 // Pages that `queries` of a sequence next to each other can see: with a window its own, the
@@ -1297,7 +1298,7 @@ int most_pages(const CacheArgs& a, int queries) {
 hipError_t launch_cache_attn(const CacheArgs& a, int D, void* ws, hipStream_t s) {
   const int rows = a.S_q * a.G;
   if (rows <= kTokenRows) {
-    const TokenPlan p = token_plan(a.B, a.Hkv, rows, D, a.M, most_pages(a, a.S_q));
+    const TokenPlan p = token_plan(a.B, a.Hkv, rows, D, a.M, most_pages(a, a.S_q), a.mask != nullptr);
     if (D == 64) launch_token<64>(a, p, (char*)ws, rows, s);
     else launch_token<128>(a, p, (char*)ws, rows, s);
   } else {

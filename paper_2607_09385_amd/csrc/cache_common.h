@@ -66,8 +66,8 @@ struct LoadArgs {
 hipError_t launch_cache_append(const StoreArgs& a, int D, hipStream_t s);
 hipError_t launch_cache_load(const LoadArgs& a, int D, hipStream_t s);
 
-// Workspace bytes of the attention for these sizes (0: none is used).
-size_t cache_attn_ws(int B, int Hq, int Hkv, int S_q, int D, int M);
+// Workspace bytes of the attention for these sizes, with a page mask or without (0: none is used).
+size_t cache_attn_ws(int B, int Hq, int Hkv, int S_q, int D, int M, bool masked);
 hipError_t launch_cache_attn(const CacheArgs& a, int D, void* ws, hipStream_t s);
 
 // Page bookkeeping (cache_pages.hip).  Pages are counted in chunks of kPageChunk.

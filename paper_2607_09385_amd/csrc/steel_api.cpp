@@ -674,9 +674,14 @@ int steel_cache_load(const uint8_t* pages, const int32_t* page_table, const int3
 }
 
 size_t steel_attn_cache_workspace_bytes(int B, int Hq, int Hkv, int S_q, int D, int max_pages) {
+  return steel_attn_cache_workspace_bytes_ex(B, Hq, Hkv, S_q, D, max_pages, 1);
+}
+
+size_t steel_attn_cache_workspace_bytes_ex(int B, int Hq, int Hkv, int S_q, int D, int max_pages,
+                                           int masked) {
   g_err.clear();
   if (check_cache_heads(B, Hq, Hkv, S_q, D, max_pages, 1) != STEEL_OK) return 0;
-  const size_t need = align256(steel::cache_attn_ws(B, Hq, Hkv, S_q, D, max_pages));
+  const size_t need = align256(steel::cache_attn_ws(B, Hq, Hkv, S_q, D, max_pages, masked != 0));
   return need > 0 ? need : 256;  // 0 stands for an error
 }
 
@@ -705,7 +710,7 @@ int steel_attn_cache(const void* q, long long q_sb, long long q_sh, long long q_
     return fail(STEEL_ERR_INVALID_ARGUMENT, "sink_blocks (%d) needs a window", sink_blocks);
   if (flags & ~STEEL_OUT_BF16)
     return fail(STEEL_ERR_INVALID_ARGUMENT, "flags may hold only STEEL_OUT_BF16 (got %d)", flags);
-  const size_t need = steel::cache_attn_ws(B, Hq, Hkv, S_q, D, max_pages);
+  const size_t need = steel::cache_attn_ws(B, Hq, Hkv, S_q, D, max_pages, block_mask != nullptr);
   if (need > 0 && (rc = check_bytes(workspace, workspace_bytes, need)) != STEEL_OK) return rc;
   steel::CacheArgs a{};
   a.q = static_cast<const __bf16*>(q);

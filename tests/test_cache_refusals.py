@@ -35,3 +35,24 @@ def test_growth_without_a_workspace():
         assert lib.steel_pages_grow_ex(F, F, F, G, F, F, F, None, sizes[1], 4, sizes[0], None, 1 << 40, None) == 1
         assert "workspace" in _lib.last_error()
     assert need(0, 2) == 0 and need(8, 0) == 0
+
+
+def test_attention_workspace_with_and_without_a_mask():
+    """The lists of live pages, 8 bytes an entry of the table and key/value head and a count a
+    list, are asked for with a mask only."""
+    lib = _lib.load()
+    need = lib.steel_attn_cache_workspace_bytes_ex
+    B, Hq, H, M = 64, 32, 8, 16384
+    masked, plain = need(B, Hq, H, 1, 128, M, 1), need(B, Hq, H, 1, 128, M, 0)
+    assert masked == lib.steel_attn_cache_workspace_bytes(B, Hq, H, 1, 128, M)
+    assert masked - plain == 8 * B * H * M + 4 * B * H and plain < 1 << 23
+    assert need(B, Hq, H, 1, 128, 24, 0) == need(B, Hq, H, 1, 128, 24, 1) == 256
+    assert need(B, Hq, H, 100, 128, M, 0) == need(B, Hq, H, 100, 128, M, 1)  # no lists are made
+    assert need(B, Hq, 3, 1, 128, M, 0) == 0 and "multiple" in _lib.last_error()
+
+    def call(mask, n):
+        return lib.steel_attn_cache(F, 0, 0, 0, F, F, F, None, mask, F, None, B, Hq, H, 1, 128, M, 9, 0.1,
+                                    1, 0, 0, 0, F, n, None)
+    assert call(F, masked - 256) == 1 and "smaller" in _lib.last_error()
+    assert call(F, plain) == 1 and "smaller" in _lib.last_error()
+    assert call(None, plain - 256) == 1 and "smaller" in _lib.last_error()
