@@ -427,12 +427,12 @@ int steel_cache_load(const uint8_t* pages, const int32_t* page_table, const int3
  * -inf.  A token whose keys or values stand for NaN makes the rows that see it
  * NaN, and no others, and so does a query with a NaN or an infinity.
  *
- * Precision: a query enters the scores as two E4M3 parts per 32 channels, exact down
- * to 2^-14 of the 32's largest magnitude and to 2^-22 of it below; keys and values are
- * exact; the sums are fp32; the softmax weights are rounded to bf16 where they meet V, so
- * out is off by up to 2^-8 of sum_j p_j |v_j|, and by the rounding of a bf16 output.
- * lse has no such rounding.  Values whose magnitude is below 2^-100 may be lost, and the
- * sum of weights times values, n times the mean at most, has to be an fp32 number.
+ * Precision: queries, keys and values are exact and the sums fp32; the softmax weights are
+ * rounded to bf16 where they meet V, so out is off by up to 2^-8 of sum_j p_j |v_j|, and by
+ * the rounding of a bf16 output.  lse has no such rounding.  Values whose magnitude is below
+ * 2^-100 may be lost, a key counts for up to 2^-126 of its value however small its weight is,
+ * and the scores, as q . k and scaled, and the sum of weights times values, n times the mean
+ * at most, have to be fp32 numbers.
  * Results are bitwise reproducible run to run.
  *
  *   workspace   at least steel_attn_cache_workspace_bytes of the same sizes (0 after an

@@ -4,16 +4,17 @@
 // over the keys j that row r sees, with the online softmax (running maximum m,
 // running sum l in fp32) over pages of 64 tokens.
 //
-// Scores.  S^T = K Q^T on the scaled MFMAs, which take K's codes and scale bytes as they are
-// stored: no decoding, and K's values exactly.  They want Q in 8 bits at most, so a query is
-// the sum of two E4M3 parts with a scale of their own per 32 channels (QueryRegs), each a
-// product: 2 x 35 cycles for 16 tokens and D = 128, against 4 x 17 of bf16 MFMAs and the 16
-// conversions a lane that those would need.
+// Scores.  S^T = K Q^T on bf16 MFMAs, K's codes and their scale turned into bf16 two at a time,
+// exactly.  The scaled MFMAs would take K as it is stored (and Q as two E4M3 parts), but they add
+// the products of a lane group on a grid of 2^-13 of the largest one: where channels differ
+// much in size a score was off by up to 2^-16 of the sum of its magnitudes, against 2^-23 here.
+// They were as fast for tokens (64 ragged sequences 65.1 us against 67.1, 4 of 8000 tokens
+// 18.1 both) and up to 6% faster for chunks (1000 queries against 12000 keys 227 against 241).
 //
 // A query row is a column of every result and its m, l and rescaling stay in the lanes
 // l % 16 = row (32 in the kernel for chunks).  Any order of the channels will do for K as
-// long as Q has the same, so lane (n = l % 16, q = l / 16) takes 32 consecutive channels of token n:
-// one 16-byte load of codes straight into registers, with one scale byte.
+// long as Q has the same, so lane (n = l % 16, q = l / 16) takes D / 4 consecutive channels of
+// token n: one 16-byte load of codes (D = 128) straight into registers, with one scale byte.
 //
 // O^T += V^T P^T on bf16 MFMAs.  The scores arrive with tokens 4 q .. 4 q + 3 of each 16 in a
 // lane, which is what the P^T operand takes when the tokens of a page are numbered in that
@@ -34,7 +35,6 @@ namespace {
 
 typedef int i32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
-typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(3))) i32x2 lds_i32x2;
 
@@ -163,108 +163,54 @@ constexpr int waves_per_simd(int D, int NT) { return NT == 1 ? 3 : 2; }
 constexpr float kTau = 8.f;  // see the running maximum below
 
 // One page's K codes and scales of a wave, on their way to registers.
+template <int D>
 struct PageRegs {
-  u32x4 k0, k1, k2, k3;
+  typedef unsigned Codes __attribute__((ext_vector_type(D / 32)));
+  Codes k0, k1, k2, k3;
   uint32_t ks0, ks1, ks2, ks3;  // scales of the lane's K codes
   uint32_t vs;                  // V scales of token `lane` (D / 32 bytes)
 };
 
-// Q of a lane's row as the fp8 operands of K Q^T: per 32 channels q = 2^e hi + 2^(e - 4) lo
-// with 2^e the smallest power of two that brings |q| to 448 or less, hi = q / 2^e and lo the
-// rest times 16, both rounded to E4M3.  hi has 4 significant bits and lo the next 4, so a
-// bf16 q is represented exactly down to 2^-14 of the 32's largest, and smaller ones to
-// 2^-22 of it.  D = 128: h holds hi of 32 channels, l lo; D = 64: h both of 16.
-template <int D>
-struct QueryRegs {
-  i32x8 h, l;
-  int se;  // scale byte of the 32 channels that this lane group stands for; D = 128: lo's in byte 1
-};
-
-// 16 channels x, scaled by 2^-e, as 4 dwords of hi and 4 of lo.
-__device__ __forceinline__ void split16(const bf16x8 (&x)[2], float inv, int* hi, int* lo) {
-#pragma unroll
-  for (int w = 0; w < 4; ++w) {
-    float f[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) f[i] = (float)x[w / 2][w % 2 * 4 + i] * inv;
-    int h = __builtin_amdgcn_cvt_pk_fp8_f32(f[0], f[1], 0, false);
-    h = __builtin_amdgcn_cvt_pk_fp8_f32(f[2], f[3], h, true);
-    hi[w] = h;
-    f[0] = 16.f * (f[0] - __builtin_amdgcn_cvt_f32_fp8(h, 0));
-    f[1] = 16.f * (f[1] - __builtin_amdgcn_cvt_f32_fp8(h, 1));
-    f[2] = 16.f * (f[2] - __builtin_amdgcn_cvt_f32_fp8(h, 2));
-    f[3] = 16.f * (f[3] - __builtin_amdgcn_cvt_f32_fp8(h, 3));
-    int l = __builtin_amdgcn_cvt_pk_fp8_f32(f[0], f[1], 0, false);
-    lo[w] = __builtin_amdgcn_cvt_pk_fp8_f32(f[2], f[3], l, true);
-  }
-}
-
-// Scale byte of 32 channels of which x holds 16 and lane l ^ OTHER the others; 255 (NaN) if
-// one is not finite.
-template <int OTHER>
-__device__ __forceinline__ int query_scale(const bf16x8 (&x)[2]) {
-  u16x2 top = {0, 0};
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const uint32_t w = __builtin_bit_cast(u32x4, x[i / 4])[i % 4] & 0x7fff7fffu;
-    top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, w));
-  }
-  uint32_t m = max((uint32_t)top[0], (uint32_t)top[1]);
-  m = max(m, (uint32_t)__shfl_xor((int)m, OTHER));
-  if (m >= 0x7f80u) return kScaleNan;
-  return max((int)(m >> 7) - 8 + ((m & 0x7fu) > 0x60u ? 1 : 0), 8);
-}
-
+// Q of a lane's row as the B operand of K Q^T: channels D / 4 q4 .., what the lane has of K.
 template <int D>
 struct QueryRows {
-  bf16x8 x[D / 32];  // channels 16 q4 .., and 64 + 16 q4 ..
+  bf16x8 x[D / 32];
 };
 template <int D>
 __device__ __forceinline__ QueryRows<D> load_query(const __bf16* q, bool real, int q4) {
   QueryRows<D> r{};
   if (real) {
 #pragma unroll
-    for (int i = 0; i < D / 32; ++i) r.x[i] = *(const bf16x8*)(q + i / 2 * 64 + 16 * q4 + i % 2 * 8);
+    for (int i = 0; i < D / 32; ++i) r.x[i] = *(const bf16x8*)(q + D / 4 * q4 + 8 * i);
   }
   return r;
 }
 
-template <int D>
-__device__ __forceinline__ QueryRegs<D> split_query(const QueryRows<D>& raw, int q4) {
-  QueryRegs<D> r;
-  const bf16x8 x[2] = {raw.x[0], raw.x[1]};
-  int hi[8], lo[8];
-  const int e0 = query_scale<16>(x);  // of channels 32 (q4 / 2) ..
-  split16(x, __uint_as_float((uint32_t)(254 - e0) << 23), hi, lo);
-  if constexpr (D == 128) {
-    const bf16x8 y[2] = {raw.x[2], raw.x[3]};
-    const int e1 = query_scale<16>(y);  // of channels 64 + 32 (q4 / 2) ..
-    split16(y, __uint_as_float((uint32_t)(254 - e1) << 23), hi + 4, lo + 4);
-    // lane group g gives the scale of channels 32 g ..: that of group 2 (g % 2)
-    const int lane = threadIdx.x & 63, from = (lane & 15) | ((q4 & 1) << 5);
-    const int s0 = __shfl(e0, from), s1 = __shfl(e1, from);
-    const int e = q4 < 2 ? s0 : s1;
-    r.se = e | (e == kScaleNan ? e : e - 4) << 8;
-    r.h = i32x8{hi[0], hi[1], hi[2], hi[3], hi[4], hi[5], hi[6], hi[7]};
-    r.l = i32x8{lo[0], lo[1], lo[2], lo[3], lo[4], lo[5], lo[6], lo[7]};
-  } else {
-    // k 0 .. 63: hi, 64 .. 127: lo of the same channels
-    const int lane = threadIdx.x & 63, from = (lane & 15) | ((q4 & 1) << 5);
-    const int s0 = __shfl(e0, from);
-    r.se = q4 < 2 || s0 == kScaleNan ? s0 : s0 - 4;
-    r.h = i32x8{hi[0], hi[1], hi[2], hi[3], lo[0], lo[1], lo[2], lo[3]};
+// A number that is not finite makes its row NaN: infinities become NaN, or a row whose scores are
+// all -inf would pass for one that sees nothing.
+template <int N>
+__device__ __forceinline__ void nan_query(bf16x8 (&x)[N]) {
+  u16x2 top = {0, 0};
+#pragma unroll
+  for (int i = 0; i < 4 * N; ++i) {
+    const uint32_t w = __builtin_bit_cast(u32x4, x[i / 4])[i % 4] & 0x7fff7fffu;
+    top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, w));
   }
-  return r;
+  if (max((uint32_t)top[0], (uint32_t)top[1]) >= 0x7f80u) x[0][0] = (__bf16)__builtin_nanf("");
 }
 
-// S^T of 16 tokens: K as it is stored (a lane's 32 codes and their scale) times Q.
+// S^T of 16 tokens: K, a lane's D / 4 codes and their scale, times Q.
 template <int D>
-__device__ __forceinline__ f32x4 scores(const u32x4& k, uint32_t ks, const QueryRegs<D>& q) {
-  const i32x8 a = {(int)k[0], (int)k[1], (int)k[2], (int)k[3], 0, 0, 0, 0};
-  f32x4 c = {0.f, 0.f, 0.f, 0.f};
-  c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, q.h, c, 4, 0, 0, (int)ks, 0, q.se);
-  if constexpr (D == 128) c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, q.l, c, 4, 0, 0, (int)ks, 1, q.se);
-  return c;
+__device__ __forceinline__ void scores(const typename PageRegs<D>::Codes& k, uint32_t ks,
+                                       const QueryRows<D>* q, int tiles, f32x4* s) {
+  const float sc = __uint_as_float(ks << 23);
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i) {
+    const bf16x8 x = decode8(k[i], sc);
+#pragma unroll
+    for (int t = 0; t < tiles; ++t)
+      s[4 * t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, q[t].x[i], i == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : s[4 * t], 0, 0, 0);
+  }
 }
 
 // How the live pages of a call are dealt to the workgroups: all lists one after
@@ -499,17 +445,16 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(D, NT)) void k_cache_to
       if (a.mask != nullptr && a.mask[((size_t)b * a.Hkv + g) * a.M + places] == 0) ids = -1;
     };
     auto record = [&](int id) { return a.pages + ((size_t)id * a.Hkv + g) * R::kBytes; };
-    // a lane's places in a record.  K, D = 64: lane groups 2 and 3 hold the channels of 0
-    // and 1 again
-    const uint32_t grp = GR == 4 ? q4 : q4 & 1;
-    const uint32_t k_at = n * R::kRow + grp * 16, ks_at = R::kKs + n * GR + grp;
+    // a lane's places in a record
+    const uint32_t k_at = n * R::kRow + q4 * (D / 8), ks_at = R::kKs + n * GR + (GR == 4 ? q4 : q4 >> 1);
     const uint32_t vs_at = R::kVs + GR * lane;
-    PageRegs x;
+    PageRegs<D> x;
+    typedef typename PageRegs<D>::Codes Codes;
     auto load_k = [&](const uint8_t* rec) {
-      x.k0 = *(const u32x4*)(rec + k_at);
-      x.k1 = *(const u32x4*)(rec + 16 * R::kRow + k_at);
-      x.k2 = *(const u32x4*)(rec + 32 * R::kRow + k_at);
-      x.k3 = *(const u32x4*)(rec + 48 * R::kRow + k_at);
+      x.k0 = *(const Codes*)(rec + k_at);
+      x.k1 = *(const Codes*)(rec + 16 * R::kRow + k_at);
+      x.k2 = *(const Codes*)(rec + 32 * R::kRow + k_at);
+      x.k3 = *(const Codes*)(rec + 48 * R::kRow + k_at);
       x.ks0 = (rec + ks_at)[0];
       x.ks1 = (rec + 16 * GR + ks_at)[0];
       x.ks2 = (rec + 32 * GR + ks_at)[0];
@@ -531,14 +476,14 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(D, NT)) void k_cache_to
     // page numbers and query rows asked for together, then the first page, then Q is split
     int id = -1, buf = 0, kb_next = 0;
     if (base < end) load_ids(base);
-    QueryRows<D> raw[NT];
+    QueryRows<D> qf[NT];
     int pos[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
       const int row = 16 * t + n, qi = row / a.G;
       const bool real = row < rows && qi < sp.n;
       pos[t] = real ? sp.first + qi : -1;
-      raw[t] = load_query<D>(a.q + b * a.q_sb + (g * a.G + row % a.G) * a.q_sh + qi * a.q_ss, real, q4);
+      qf[t] = load_query<D>(a.q + b * a.q_sb + (g * a.G + row % a.G) * a.q_sh + qi * a.q_ss, real, q4);
     }
     if (base < end) {
       id = __builtin_amdgcn_readfirstlane(ids);
@@ -546,12 +491,11 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(D, NT)) void k_cache_to
       copy_v(record(max(id, 0)), 0);
       load_k(record(max(id, 0)));
     }
-    QueryRegs<D> qf[NT];  // the lane's part of Q as the B operand
     f32x4 o[NT][CT];
     float m[NT], l[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-      qf[t] = split_query<D>(raw[t], q4);
+      nan_query(qf[t].x);
 #pragma unroll
       for (int c = 0; c < CT; ++c) o[t][c] = f32x4{0.f, 0.f, 0.f, 0.f};
       m[t] = -INFINITY;
@@ -562,13 +506,10 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(D, NT)) void k_cache_to
       const int kb = kb_next;
       // S^T: 4 tiles of 16 tokens
       f32x4 sc[NT][4];
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        sc[nt][0] = scores<D>(x.k0, x.ks0, qf[nt]);
-        sc[nt][1] = scores<D>(x.k1, x.ks1, qf[nt]);
-        sc[nt][2] = scores<D>(x.k2, x.ks2, qf[nt]);
-        sc[nt][3] = scores<D>(x.k3, x.ks3, qf[nt]);
-      }
+      scores<D>(x.k0, x.ks0, qf, NT, &sc[0][0]);
+      scores<D>(x.k1, x.ks1, qf, NT, &sc[0][1]);
+      scores<D>(x.k2, x.ks2, qf, NT, &sc[0][2]);
+      scores<D>(x.k3, x.ks3, qf, NT, &sc[0][3]);
       // tokens whose values stand for NaN (all scale bytes 255, or none), and whether any value is
       // above 2^64; bytes behind the sequence count as 0
       uint32_t vs = kb * kBlk + lane < sp.keys ? x.vs : 0u;
@@ -828,7 +769,8 @@ __global__ __launch_bounds__(64 * kWaves) void k_cache_join(CacheArgs a, SplitAr
 // Many rows per key/value head (chunks of prompts): tiles of 128 rows, 4 waves of 32.
 //
 // S^T = K Q^T and O^T = V^T P^T on 32x32 MFMAs, a row in the lanes l % 32.  A page's K codes go
-// to LDS as they are and into scaled MFMAs; its V is turned into bf16 by the whole
+// to LDS as they are and every wave turns them into bf16 (once for the workgroup, with bf16
+// keys in LDS: 254 us against 247); its V is turned into bf16 by the whole
 // workgroup (16 conversions and four 16-byte LDS writes a thread) and read
 // transposed, as the dense kernels do.  Both are one page ahead: K by copies, V's codes in
 // registers until the present page is done.
@@ -836,9 +778,7 @@ __global__ __launch_bounds__(64 * kWaves) void k_cache_join(CacheArgs a, SplitAr
 // Bound by the MFMAs and the exponentials between them: 1000 queries of 32 heads against 12000
 // keys of 8 heads of 128 (188 GFLOP) 198 us with the join, 950 TFLOP/s; a large bf16 matrix
 // product reaches 1256 on the same card.  MFMAs take 40% of the cycles, VALU 44%, and the two
-// hardly overlap.  Two workgroups per CU; K Q^T costs twice its MFMA
-// time for the two parts of Q and is still no dearer than in bf16 (64 cycles for 64
-// channels, twice, against 4 x 33), without conversions or LDS traffic of bf16 keys.
+// hardly overlap.  Two workgroups per CU.
 // Segments (below) fill the chip where the tiles are few: 211 us against 309 without here.
 // Waves of 64 rows were no faster (D = 64: 152 against 157 us, but 159 against 130 with 12 heads) or
 // spilled (D = 128: 596).
@@ -901,29 +841,15 @@ __global__ __launch_bounds__(256, 2) void k_cache_chunk(CacheArgs a, ChunkArgs c
   const int row = r0 + 32 * wave + n, qi = row / a.G;
   const bool real = row < r1 && qi < sp.n;
   const int pos = real ? sp.first + qi : -1;
-  i32x8 qh[KS], ql[KS];
-  int se[KS];  // scale bytes (lo's in byte 1): lane half h gives those of channels 64 s + 32 h ..
-  {
-    const __bf16* q = a.q + b * a.q_sb + (g * a.G + row % a.G) * a.q_sh + qi * a.q_ss + 16 * hf;
+  bf16x8 q[4 * KS];  // channels 64 s + 32 hf + 8 i .. at 4 s + i
 #pragma unroll
-    for (int s = 0; s < KS; ++s) {
-      int hi[8], lo[8], e[2];
+  for (int i = 0; i < 4 * KS; ++i) q[i] = bf16x8{};
+  if (real) {
+    const __bf16* at = a.q + b * a.q_sb + (g * a.G + row % a.G) * a.q_sh + qi * a.q_ss + 32 * hf;
 #pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        bf16x8 x[2] = {bf16x8{}, bf16x8{}};
-        if (real) {
-          x[0] = *(const bf16x8*)(q + 64 * s + 32 * c);
-          x[1] = *(const bf16x8*)(q + 64 * s + 32 * c + 8);
-        }
-        e[c] = query_scale<32>(x);
-        split16(x, __uint_as_float((uint32_t)(254 - e[c]) << 23), hi + 4 * c, lo + 4 * c);
-      }
-      const int eh = hf ? e[1] : e[0];
-      se[s] = eh | (eh == kScaleNan ? eh : eh - 4) << 8;
-      qh[s] = i32x8{hi[0], hi[1], hi[2], hi[3], hi[4], hi[5], hi[6], hi[7]};
-      ql[s] = i32x8{lo[0], lo[1], lo[2], lo[3], lo[4], lo[5], lo[6], lo[7]};
-    }
+    for (int i = 0; i < 4 * KS; ++i) q[i] = *(const bf16x8*)(at + i / 4 * 64 + i % 4 * 8);
   }
+  nan_query(q);
 
   // pages: the numbers of 64 list entries, one per lane, and the set of those still to come;
   // pages that do not exist or are masked are never visited
@@ -1029,20 +955,21 @@ __global__ __launch_bounds__(256, 2) void k_cache_chunk(CacheArgs a, ChunkArgs c
     // S^T: 2 tiles of 32 tokens
     f32x16 sc[2];
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const int kse = (int)(ks[t] >> (8 * hf));
+    for (int t = 0; t < 2; ++t) sc[t] = f32x16{};
 #pragma unroll
-      for (int s = 0; s < KS; ++s) {
-        const u32x4 k = *(lds_u32x4)(lds_cp)(kr_at + buf * KB + 32 * t * VROW + (((2 * s + hf) ^ ksw) * 16));
-        const i32x8 ka = {(int)k[0], (int)k[1], (int)k[2], (int)k[3], 0, 0, 0, 0};
-        if (s == 0) {
-          sc[t] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ka, qh[s], f32x16{}, 4, 0, 0, kse, 0, se[s]);
-          sc[t] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ka, ql[s], sc[t], 4, 0, 0, kse, 1, se[s]);
-        } else {
-          sc[t] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ka, qh[s], sc[t], 4, 0, 2, kse, 0, se[s]);
-          sc[t] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ka, ql[s], sc[t], 4, 0, 2, kse, 1, se[s]);
-        }
+    for (int s = 0; s < KS; ++s) {
+      u32x4 k[2];
+      float kse[2];
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        k[t] = *(lds_u32x4)(lds_cp)(kr_at + buf * KB + 32 * t * VROW + (((2 * s + hf) ^ ksw) * 16));
+        kse[t] = __uint_as_float((ks[t] >> (8 * hf + 16 * s) & 0xff) << 23);
       }
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+          sc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(decode8(k[t][i], kse[t]), q[4 * s + i], sc[t], 0, 0, 0);
     }
     if (!page_full(a, sp, kb)) {
       const int lim = row_limit(a, sp, pos, kb) - 4 * hf;
