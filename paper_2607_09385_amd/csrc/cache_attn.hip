@@ -224,9 +224,10 @@ __device__ __forceinline__ void scores(const typename PageRegs<D>::Codes& k, uin
 // one list only.  64 lists of 51 pages: 22.4 us against 25.5 as below, 8 of 512: 24.7 against
 // 29.3; but 128 of 512: 124 against 117, for the workgroups left without a unit.
 // Lists of nearly one length (the longest up to 9/8 of the mean) of which two or three a CU
-// fill all but a few CUs (448 .. 512, 736 .. 768): a workgroup each, nothing is joined.  512 of
-// 32 pages: 40.9 us against 46.0, of 128: 115.8 against 124.4; but 384 of 128 pages: 104
-// against 98, 576 of 128 with D = 64: 72 against 65.
+// fill all but a quarter of the CUs' last places (448 .. 512, 704 .. 768): a workgroup each, nothing
+// is joined.  456 of 32 pages: 36.6 us against 41.5, 512 40.9 against 46.0, 704 51.5 against 55.8;
+// of 128 pages 456 105 against 114, 512 115.8 against 124.4; but 384 of 128 pages: 104 against 98,
+// 576 of 128 with D = 64: 72 against 65.
 // Else a list counts `cost` units beyond its pages for what it takes besides (page
 // numbers, Q, the first page's latency, the joined states): up to 10, but no more than a
 // quarter of what a workgroup gets (64 ragged sequences 82.6 us, with 8 85.2, with 12 83.5).
@@ -292,7 +293,7 @@ __device__ __forceinline__ Deal make_deal(const CacheArgs& a, const SplitArgs& s
     const int u = (tp + sa.groups - tl - 1) / (sa.groups - tl);  // the lists' last units fill at most tl more
     d.cost = 0;
     d.unit = d.fill = max((u + kWaves - 1) / kWaves * kWaves, kWaves);
-  } else if (tl > 256 && tl <= sa.groups && (tl + 32) / 256 * 256 >= tl && (long long)top * tl <= (long long)tp + tp / 8) {
+  } else if (tl > 256 && tl <= sa.groups && (tl + 64) / 256 * 256 >= tl && (long long)top * tl <= (long long)tp + tp / 8) {
     d.cost = 0;
     d.unit = d.fill = top;
   } else {
