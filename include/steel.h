@@ -361,7 +361,9 @@ int steel_attn_fwd_noalloc(const void* q, const void* k, const void* v,
  * counts and page numbers are device memory and are read by the kernels: a
  * page number outside [0, n_pages) is a page that does not exist (nothing is
  * written to it, no key of it is visible), a length outside [0, 64 max_pages]
- * counts as the nearer end of it where keys are read or pages held.
+ * counts as the nearer end of it where keys are read or pages held.  A caller that writes a
+ * smaller length (drafted tokens that were rejected) lowers the counts of the entries behind
+ * the new end itself: the calls below count what a row holds when they run.
  *
  * n_new int32 [B], device, or NULL: how many of the S tokens (or S_q queries)
  * of a padded batch sequence b has, at the front of its S (clamped to [0, S];
@@ -433,7 +435,9 @@ int steel_cache_load(const uint8_t* pages, const int32_t* page_table, const int3
  * 2^-100 may be lost, a key counts for up to 2^-126 of its value however small its weight is,
  * and the scores, as q . k and scaled, and the sum of weights times values, n times the mean
  * at most, have to be fp32 numbers.
- * Results are bitwise reproducible run to run.
+ * Results are bitwise reproducible run to run.  Which bits a row gets inside these bounds may
+ * depend on the other rows of its call and on what its pages hold beyond its own keys (a
+ * key that only a later query sees): rows share the steps of their running maxima.
  *
  *   workspace   at least steel_attn_cache_workspace_bytes of the same sizes (0 after an
  *               argument error); where that is 256 none is used and it may be NULL.

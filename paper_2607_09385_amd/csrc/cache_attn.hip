@@ -23,7 +23,10 @@
 // sum, so they go into the weights: p_rj 2^e_jg is formed once per group of 32 channels (an
 // addition to the exponents: exact), and the codes alone are turned into bf16.  Weights are
 // rounded to bf16, the precision of the MFMA's operands (off by 2^-8 of each weight at most, in
-// either direction); l adds them before that rounding.
+// either direction), as in this library's dense calls; l adds them before that rounding.  A
+// second bf16 part of each weight would take the error of a bf16 output from 0.0020-0.0023 of it to
+// the 0.0017 of its own rounding, for 8 to 15% of the time of tokens (16 x 32768 112 us to 121, 64 x
+// 3000 42 to 48, 32 rows 53 to 74) and 20% of chunks (226 to 278).
 //
 // A page id outside the pool is a page without visible keys; keys behind the
 // sequence's length are never visible, whatever their bytes.
@@ -273,7 +276,9 @@ __device__ __forceinline__ int set_pages(const CacheArgs& a, const SplitArgs& sa
 }
 
 // Every wave finds it by itself, lane by lane 64 sets at a time: no exchange, and where there
-// are no more sets than that one load.
+// are no more sets than that one load.  More are read three times over, a latency each: calls
+// of one-page lists take 8.8 us with 64 sequences, 37 with 512 and 151 with 4096 (18 and 62
+// where each list is a workgroup's), under a page mask 17 us with 512 lists, 47 with 2048, 167 with 8192.
 __device__ __forceinline__ Deal make_deal(const CacheArgs& a, const SplitArgs& sa, int rows) {
   const int lane = threadIdx.x & 63, sets = deal_sets(a, sa), heads = sa.counts != nullptr ? 1 : a.Hkv;
   const int n0 = lane < sets ? set_pages(a, sa, lane, rows) : 0;
@@ -361,7 +366,7 @@ __device__ __forceinline__ void store_row(const CacheArgs& a, const Span& sp, in
 // are on their way while a wave computes, 12 waves a CU, 104 KB.  16 sequences of 32768
 // tokens, 8 heads of 128 (570 MB): 115 us, 5.0 TB/s; a kernel that only reads these records in
 // this order reaches 5.8.  64 ragged sequences of up to 32768 (374 MB): 83 us, 4.5 TB/s, for
-// the lists that begin and end inside workgroups.  4 sequences of 8000 (35 MB): 12 us, bound by
+// the lists that begin and end inside workgroups.  4 sequences of 8000 (35 MB): 14 us cold, bound by
 // a chain of latencies: lengths, page numbers, 2 pages a wave, the joined states.  A third
 // wave per SIMD is worth more than registers: 2 waves, 73 us against 68 for 64 sequences of
 // 4000 on average; 4 waves spill (150 us and more).  With NT = 2 two waves fit.
@@ -771,16 +776,17 @@ __global__ __launch_bounds__(64 * kWaves) void k_cache_join(CacheArgs a, SplitAr
 //
 // S^T = K Q^T and O^T = V^T P^T on 32x32 MFMAs, a row in the lanes l % 32.  A page's K codes go
 // to LDS as they are and every wave turns them into bf16 (once for the workgroup, with bf16
-// keys in LDS: 254 us against 247); its V is turned into bf16 by the whole
+// keys in LDS: 254 us against 241); its V is turned into bf16 by the whole
 // workgroup (16 conversions and four 16-byte LDS writes a thread) and read
 // transposed, as the dense kernels do.  Both are one page ahead: K by copies, V's codes in
 // registers until the present page is done.
 //
 // Bound by the MFMAs and the exponentials between them: 1000 queries of 32 heads against 12000
-// keys of 8 heads of 128 (188 GFLOP) 198 us with the join, 950 TFLOP/s; a large bf16 matrix
-// product reaches 1256 on the same card.  MFMAs take 40% of the cycles, VALU 44%, and the two
+// keys of 8 heads of 128 (188 GFLOP) 213 us with the join, 880 TFLOP/s; a large bf16 matrix
+// product reaches 1256 on the same card.  MFMAs take 39% of the cycles, VALU 53%, and the two
 // hardly overlap.  Two workgroups per CU.
-// Segments (below) fill the chip where the tiles are few: 211 us against 309 without here.
+// Segments (below) fill the chip where the tiles are few: 239 us against 283 without here (random
+// codes), 64 queries against 16000 keys 55 against 355.
 // Waves of 64 rows were no faster (D = 64: 152 against 157 us, but 159 against 130 with 12 heads) or
 // spilled (D = 128: 596).
 struct ChunkArgs {
@@ -798,8 +804,8 @@ __device__ __forceinline__ int tile_segments(const ChunkArgs& ca, int count) {
 }
 
 // Workgroup -> (unit, tile, segment).  With a multiple of 8 units each keeps to one XCD,
-// whose L2 then holds its keys and values (2048 queries of 32 heads, 4096 keys: 139 us against
-// 160; 512 queries, 16384 keys 171 against 174); a unit's heaviest tiles come first.
+// whose L2 then holds its keys and values (2048 queries of 32 heads, 4096 keys: 143 us against
+// 161; 512 queries, 16384 keys 177 against 179); a unit's heaviest tiles come first.
 __device__ __forceinline__ void chunk_item(const CacheArgs& a, const ChunkArgs& ca, int* unit, int* tile,
                                            int* seg) {
   const int per = ca.tiles * ca.ns, units = a.B * a.Hkv, i = blockIdx.x;
@@ -1101,8 +1107,8 @@ ChunkPlan chunk_plan(int B, int Hkv, int rows, int D, int pages) {
   const long long items = (long long)B * Hkv * p.tiles;
   long long ns = (512 + items - 1) / items;  // two workgroups per CU
   // A segment saves its share of a tile's pages and costs 64 KB or 128 KB written and read back, the
-  // more the more tiles do so: 8 pages at least, 27 with 384 tiles.  With 8 always, 384 tiles of 10
-  // pages took 49 us (31), 376 of up to 36 82 us (71), 256 of 9 30 us (19).
+  // more the more tiles do so: 8 pages at least, 27 with 384 tiles.  With 8 always, 376 tiles of up
+  // to 36 pages take 88 us (67), 436 of up to 32 54 us (48); 32 of 188 the same.
   p.least = 8 + (int)(items < 512 ? items / 20 : 0);
   const long long most = pages / p.least > 1 ? pages / p.least : 1;
   p.ns = (int)(ns < most ? ns : most);
@@ -1124,8 +1130,8 @@ void launch_chunk(const CacheArgs& a, const ChunkPlan& p, void* ws, hipStream_t 
 }
 
 // The live pages of every list, one workgroup each: the pages of the span that exist and
-// whose mask byte is set, in order.  A tenth of 64 lists of 512: 4.7 us, latency bound, and the
-// attention 19.9; where k_cache_token skipped the others itself it took 49.
+// whose mask byte is set, in order.  A tenth of 64 lists of 512: 5.0 us, latency bound, and the
+// attention 13.9; where k_cache_token skipped the others itself it took 49.
 __global__ __launch_bounds__(256) void k_cache_lists(CacheArgs a, int rows, int2* list, int* counts) {
   __shared__ int found[2][4];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = blockIdx.x, b = i / a.Hkv;
@@ -1205,8 +1211,9 @@ void launch_token(const CacheArgs& a, const TokenPlan& p, char* ws, int rows, hi
 }
 
 // Up to 32 rows of a key/value head go to k_cache_token, which streams pages past the rows; more to
-// k_cache_chunk, whose tiles of 128 share them.  32 rows, 8 sequences of 16000 tokens: 50 us against
-// 84 (D = 128), 36 against 61 (D = 64); one sequence 30 against 38.  More than 32 rows would take a
+// k_cache_chunk, whose tiles of 128 share them.  32 rows, 8 heads of 128: 8 sequences of 16384 tokens
+// 52 us against 89, one of 32768 29 against 62, 64 of 200 to 8100 114 against 236 (D = 64: 83
+// against 169).  More than 32 rows would take a
 // third tile of accumulators, which do not fit into registers beside two.
 constexpr int kTokenRows = 32;
 

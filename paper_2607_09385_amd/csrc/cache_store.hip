@@ -12,9 +12,9 @@
 // Memory bound: a lane takes 8 channels (16 bytes of bf16, 4 of codes), the
 // lanes of a vector are neighbours and so are the tokens of a head, so a wave
 // reads 1 KiB and writes 256 bytes of codes contiguously per tensor.  Prompts of 8,586 tokens in
-// all (8 heads of 128) out of a cold cache: written in 17.5 us, read back into 4 x 8192 padded rows
-// in 25.7; 160 MB together at 3.7 TB/s, where a plain copy of as many bytes takes 46 us.
-// One token of 64 sequences: 4.9 us, a launch and two dependent loads.
+// all (8 heads of 128) out of a cold cache: written in 15.2 us, read back into 4 x 8192 padded rows
+// in 20.4; 160 MB together at 4.5 TB/s, where a plain copy of as many bytes takes 27 us.
+// One token of 64 sequences: 4.8 us, a launch and two dependent loads.
 #include "cache_common.h"
 
 namespace steel {
