@@ -25,7 +25,7 @@
 // rounded to bf16, the precision of the MFMA's operands (off by 2^-8 of each weight at most, in
 // either direction), as in this library's dense calls; l adds them before that rounding.  A
 // second bf16 part of each weight would take the error of a bf16 output from 0.0020-0.0023 of it to
-// the 0.0017 of its own rounding, for 8 to 15% of the time of tokens (16 x 32768 112 us to 121, 64 x
+// the 0.0017 of its own rounding, for 8 to 18% of the time of tokens (16 x 32768 112 us to 121, 64 x
 // 3000 42 to 48, 32 rows 53 to 74) and 20% of chunks (226 to 278).
 //
 // A page id outside the pool is a page without visible keys; keys behind the
