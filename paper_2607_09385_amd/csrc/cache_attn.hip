@@ -202,17 +202,17 @@ __device__ __forceinline__ void nan_query(bf16x8 (&x)[N]) {
   if (max((uint32_t)top[0], (uint32_t)top[1]) >= 0x7f80u) x[0][0] = (__bf16)__builtin_nanf("");
 }
 
-// S^T of 16 tokens: K, a lane's D / 4 codes and their scale, times Q.
-template <int D>
+// S^T of tokens 16 i ..: K, a lane's D / 4 codes and their scale, times Q.
+template <int D, int NT>
 __device__ __forceinline__ void scores(const typename PageRegs<D>::Codes& k, uint32_t ks,
-                                       const QueryRows<D>* q, int tiles, f32x4* s) {
+                                       const QueryRows<D> (&q)[NT], f32x4 (&s)[NT][4], int i) {
   const float sc = __uint_as_float(ks << 23);
 #pragma unroll
-  for (int i = 0; i < D / 32; ++i) {
-    const bf16x8 x = decode8(k[i], sc);
+  for (int c = 0; c < D / 32; ++c) {
+    const bf16x8 x = decode8(k[c], sc);
 #pragma unroll
-    for (int t = 0; t < tiles; ++t)
-      s[4 * t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, q[t].x[i], i == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : s[4 * t], 0, 0, 0);
+    for (int t = 0; t < NT; ++t)
+      s[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, q[t].x[c], c == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : s[t][i], 0, 0, 0);
   }
 }
 
@@ -512,10 +512,10 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(D, NT)) void k_cache_to
       const int kb = kb_next;
       // S^T: 4 tiles of 16 tokens
       f32x4 sc[NT][4];
-      scores<D>(x.k0, x.ks0, qf, NT, &sc[0][0]);
-      scores<D>(x.k1, x.ks1, qf, NT, &sc[0][1]);
-      scores<D>(x.k2, x.ks2, qf, NT, &sc[0][2]);
-      scores<D>(x.k3, x.ks3, qf, NT, &sc[0][3]);
+      scores<D, NT>(x.k0, x.ks0, qf, sc, 0);
+      scores<D, NT>(x.k1, x.ks1, qf, sc, 1);
+      scores<D, NT>(x.k2, x.ks2, qf, sc, 2);
+      scores<D, NT>(x.k3, x.ks3, qf, sc, 3);
       // tokens whose values stand for NaN (all scale bytes 255, or none), and whether any value is
       // above 2^64; bytes behind the sequence count as 0
       uint32_t vs = kb * kBlk + lane < sp.keys ? x.vs : 0u;
